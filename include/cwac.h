@@ -446,6 +446,58 @@ cwac_status qlinear_w4a16_cwac_forward(const uint16_t *x, int64_t ldx, const voi
                                        void *out, int64_t ldo, void *stream);
 
 /* ------------------------------------------------------------------------- */
+/* Microscaled 4-bit floating point (weights and activations) with the         */
+/* compensation in the epilogue                                                */
+/* ------------------------------------------------------------------------- */
+/* The block-scaled format of the card's 10 PFLOP/s matrix instructions: 32 consecutive values of a row share a power of two,
+ * an element is a number of 4 bits.  A 4-bit layer needs the per-channel compensation of Sec. 3.3 most; it is fitted
+ * (fp32 output, cwac_calibrate_stats, cwac_solve) and folded (cwac_fold_weight_only) as for the INT4 layer above.
+ *
+ * Format of a matrix [rows, k] (k % 32 == 0):
+ *   codes   uint8 [rows, k / 2], pitch ldc BYTES: value 2 j of a row in the low half of byte j, value 2 j + 1 in the high
+ *           half; sign bit and magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6 (E2M1)
+ *   scales  uint8 [ceil(k / 256)][rows][8]: byte e + 127 of block b (values 32 b .. 32 b + 31) of row r at
+ *           [b / 8][r][b % 8]; cwac_mx4_scale_bytes(rows, k) bytes; bytes of blocks beyond k are zero (the product
+ *           relies on it)
+ *   value = code * 2^e; scale byte 255: the block's values are NaN
+ * Limits: 1 <= rows <= 2^31 - 1 in the product (rows >= 0 in the conversions), 32 <= k <= 262144; codes 16-byte aligned,
+ * ldc >= k / 2, ldc % 16 == 0; scales 8-byte aligned. */
+enum { CWAC_MX4_BLOCK = 32, CWAC_MX4_PANEL = 256 };
+enum { CWAC_OUT_BF16 = 4 }; /* bfloat16 values cross this interface as their bit patterns, like binary16 ones */
+
+/* Bytes of the scales of a [rows, k] matrix; 0 for sizes out of range. */
+size_t cwac_mx4_scale_bytes(int64_t rows, int32_t k);
+
+/* e = clamp(floor(log2(max |x|)) - 2, -127, 127) over the block (all zeros: -127);
+ * code = the E2M1 number nearest to x / 2^e, ties to the even code, magnitudes above 6 to 6.  A block that holds a NaN or an
+ * infinity gets scale byte 255 and codes 0.
+ *   x       device [rows, k] of x_type CWAC_OUT_FP32, CWAC_OUT_FP16 or CWAC_OUT_BF16; pitch ldx elements; 16-byte
+ *           aligned, ldx * sizeof(element) % 16 == 0
+ *   rows >= 0 (0 is a no-op) */
+cwac_status cwac_mx4_quantize(const void *x, int32_t x_type, int64_t ldx, int64_t rows, int32_t k, uint8_t *codes,
+                              int64_t ldc, uint8_t *scales, void *stream);
+
+/* The values that the codes stand for (NaN where the scale byte is 255): exact in fp32 and bfloat16, rounded to nearest even
+ * (beyond 65504: infinity) in binary16.  out: device [rows, k] of out_type, pitch ldo, aligned like x above. */
+cwac_status cwac_mx4_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scales, int64_t rows, int32_t k, void *out,
+                                int32_t out_type, int64_t ldo, void *stream);
+
+/* out = epilogue(x * w^T) of two matrices in this format, on the matrix cores:
+ *   acc = sum_k x[m, k] * w[n, k]       exact products, fp32 accumulation (order unspecified)
+ *   u   = acc * mult[n]                 mult == NULL: multiplier 1
+ *   u   = u + fbias[n]                  fbias == NULL: no constant  (single fp32 operations)
+ *   out = u rounded to nearest even to out_kind: CWAC_OUT_FP32 (calibration forward), CWAC_OUT_FP16 or CWAC_OUT_BF16
+ * A block of NaN in row m of x or row n of w makes the outputs of that row or column NaN.
+ *   x_codes, x_scales  [m, k] (activations), w_codes, w_scales [n, k] (weights, nn.Linear layout); ldx, ldw bytes, <= 2^24
+ *   m >= 1, n >= 1
+ *   mult, fbias        device fp32 [n] or NULL
+ *   out                device [m, n], pitch ldo elements; 16-byte aligned rows take whole-line stores, others element-wise ones */
+cwac_status qlinear_mx4_cwac_forward(const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales, const uint8_t *w_codes,
+                                     int64_t ldw, const uint8_t *w_scales, int64_t m, int32_t n, int32_t k,
+                                     const float *mult, const float *fbias, int32_t out_kind, void *out, int64_t ldo,
+                                     void *stream);
+
+/* ------------------------------------------------------------------------- */
 /* Glue of a Transformer block between its W8A8 linear layers                  */
 /* ------------------------------------------------------------------------- */
 /* Per-layer compensation exists because the rest of the block is non-linear (Sec. 3.2); the

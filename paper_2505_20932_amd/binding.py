@@ -23,8 +23,9 @@ LIB_PATH = os.environ.get("CWAC_LIB") or os.path.join(_PKG, "libcwac_hip.so")
 
 CWAC_OK = 0
 CWAC_EPI_INT_OFFSET, CWAC_EPI_FP_BIAS = 0, 1
-CWAC_OUT_INT8, CWAC_OUT_FP32, CWAC_OUT_INT32, CWAC_OUT_FP16 = 0, 1, 2, 3
+CWAC_OUT_INT8, CWAC_OUT_FP32, CWAC_OUT_INT32, CWAC_OUT_FP16, CWAC_OUT_BF16 = 0, 1, 2, 3, 4
 CWAC_W4_GROUP = 128
+CWAC_MX4_BLOCK, CWAC_MX4_PANEL = 32, 256
 # cwac_tuning.kernel / .shape
 CWAC_KERNEL_AUTO, CWAC_KERNEL_DIRECT_LDS, CWAC_KERNEL_SPLIT_K = 0, 1, 2
 CWAC_KERNEL_GENERIC_64, CWAC_KERNEL_GENERIC_128, CWAC_KERNEL_GENERIC_256 = 64, 128, 256
@@ -48,6 +49,7 @@ EXPORTS = (
     "qlinear_cwac_calibrate_fused_ex", "qlinear_cwac_forward_fixed_point_ex",
     "qlinear_w4a16_cwac_forward_ex", "cwac_forward_kernel_for",
     "cwac_static_scratch_bytes", "cwac_calibrate_stats_static",
+    "cwac_mx4_scale_bytes", "cwac_mx4_quantize", "cwac_mx4_dequantize", "qlinear_mx4_cwac_forward",
 )
 
 
@@ -166,6 +168,10 @@ def lib() -> C.CDLL:
             "vit_block_w8a8_forward": (i32, [C.POINTER(vit_block_params), vp, vp, vp, sz, vp]),
             "vit_encoder_w8a8_forward": (i32, [C.POINTER(vit_block_params), i32, vp, vp, vp, sz, vp]),
         }
+        sig["cwac_mx4_scale_bytes"] = (sz, [i64, i32])
+        sig["cwac_mx4_quantize"] = (i32, [vp, i32, i64, i64, i32, vp, i64, vp, vp])
+        sig["cwac_mx4_dequantize"] = (i32, [vp, i64, vp, i64, i32, vp, i32, i64, vp])
+        sig["qlinear_mx4_cwac_forward"] = (i32, [vp, i64, vp, vp, i64, vp, i64, i32, i32, vp, vp, i32, vp, i64, vp])
         sig["cwac_calibrate_stats_first"] = sig["cwac_calibrate_stats"]
         sig["cwac_static_scratch_bytes"] = (sz, [])
         sig["cwac_calibrate_stats_static"] = (i32, [vp, i64, vp, i64, i64, i32, vp, vp])
@@ -526,6 +532,75 @@ def qlinear_w4a16_cwac_forward(x: torch.Tensor, packed_w: torch.Tensor, packed_s
     else:
         _check(lib().qlinear_w4a16_cwac_forward_ex(*args, _tun(tuning), _stream(stream)),
                "qlinear_w4a16_cwac_forward_ex")
+
+
+# --------------------------------------------------------------------------- microscaled 4-bit floating point
+_KIND = {torch.float32: CWAC_OUT_FP32, torch.float16: CWAC_OUT_FP16, torch.bfloat16: CWAC_OUT_BF16,
+         torch.int8: CWAC_OUT_INT8}
+
+
+def _device_of(*tensors):
+    """The device that all of a call's tensors are on (None among them: left out)."""
+    dev = None
+    for t in tensors:
+        if t is not None:
+            assert t.is_cuda, "device tensor expected"
+            assert dev is None or t.device == dev, "the tensors of a call are on one device"
+            dev = t.device
+    return dev
+
+
+def _call(name: str, dev, stream, *args):
+    """One call on `dev` (which need not be the current device) and its current stream, or on `stream`."""
+    fn = getattr(lib(), name)
+    if dev.index == torch.cuda.current_device():
+        status = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, _stream(stream))
+    _check(status, name)
+
+
+def cwac_mx4_scale_bytes(rows: int, k: int) -> int:
+    return int(lib().cwac_mx4_scale_bytes(rows, k))
+
+
+def _mx4(codes: torch.Tensor, scales: torch.Tensor, rows: int, k: int):
+    """Pointer and pitch of the codes, pointer of the scales of a [rows, k] matrix in the microscaled format."""
+    assert codes.dtype == torch.uint8 and codes.shape == (rows, k // 2)
+    assert scales.dtype == torch.uint8 and scales.is_contiguous()
+    assert scales.shape == (-(-k // CWAC_MX4_PANEL), rows, 8)
+    return _ptr(codes), _rowmajor(codes), _ptr(scales)
+
+
+def cwac_mx4_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None):
+    """x float32 / float16 / bfloat16 [rows, k]; codes uint8 [rows, k/2]; scales uint8 [ceil(k/256), rows, 8]."""
+    dev = _device_of(x, codes, scales)
+    rows, k = x.shape
+    cp, ldc, sp = _mx4(codes, scales, rows, k)
+    _call("cwac_mx4_quantize", dev, stream, _ptr(x), _KIND[x.dtype], _rowmajor(x), rows, k, cp, ldc, sp)
+
+
+def cwac_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, stream=None):
+    """The values of the codes into out float32 / float16 / bfloat16 [rows, k]."""
+    dev = _device_of(out, codes, scales)
+    rows, k = out.shape
+    cp, ldc, sp = _mx4(codes, scales, rows, k)
+    _call("cwac_mx4_dequantize", dev, stream, cp, ldc, sp, rows, k, _ptr(out), _KIND[out.dtype], _rowmajor(out))
+
+
+def qlinear_mx4_cwac_forward(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor,
+                             w_scales: torch.Tensor, mult, fbias, out: torch.Tensor, stream=None):
+    """Codes and scales as cwac_mx4_quantize leaves them; mult, fbias float32 [n] or None; out float32 / float16 /
+    bfloat16 [m, n]."""
+    dev = _device_of(x_codes, x_scales, w_codes, w_scales, mult, fbias, out)
+    (m, n), k = out.shape, 2 * x_codes.shape[1]
+    xp, ldx, xs = _mx4(x_codes, x_scales, m, k)
+    wp, ldw, ws = _mx4(w_codes, w_scales, n, k)
+    for t in (mult, fbias):
+        assert t is None or (t.dtype == torch.float32 and t.shape == (n,) and t.is_contiguous())
+    _call("qlinear_mx4_cwac_forward", dev, stream, xp, ldx, xs, wp, ldw, ws, m, n, k, _ptr(mult), _ptr(fbias),
+          _KIND[out.dtype], _ptr(out), _rowmajor(out))
 
 
 # --------------------------------------------------------------------------- block glue

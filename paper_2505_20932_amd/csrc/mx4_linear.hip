@@ -1,0 +1,313 @@
+// Linear layer on microscaled 4-bit operands (E2M1 codes, a power of two per 32 values of a row) with the CWAC epilogue:
+//   y[m, n] = (sum over blocks b of 2^(ex[m, b] + ew[n, b]) * sum_i cx[m, 32 b + i] cw[n, 32 b + i]) * mult[n] + fbias[n].
+// The block-scaled matrix instructions take both codes and scale bytes: a lane's operand is 16 bytes of codes = one
+// block of one row, and its scale is one byte of a register that the instruction selects.  So the codes' way through the kernel is that of an
+// int8 layer of half the K, and the scales ride beside them.
+//
+// Which block of a K step a lane holds is free as long as both operands agree (the sum has no order), so each lane group takes
+// consecutive blocks over the steps of a 256-value panel: its scale bytes are then consecutive bytes of the
+// panel's eight, one load for all of the panel's steps.
+//
+// K that is no multiple of 256: the last panel's codes beyond K are whatever lies there (the next row, the gap between rows, zeros
+// behind the last row), finite numbers all of them, and their scale bytes are zero on both sides: products of
+// 2^-254 or less, far below half an ulp of any fp32 sum that is not zero and zero when rounded to fp32 by themselves.
+#include <type_traits>
+
+#include "mx4.h"
+#include "qlinear_common.h"
+
+namespace cwac {
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int v8i __attribute__((ext_vector_type(8)));
+
+#define CWAC_LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
+#define CWAC_GLOBAL_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
+
+struct Mx4Params {
+  const uint8_t *x, *w, *xs, *ws;
+  int64_t ldx, ldw, ldo, m;
+  int n, k;
+  const float *mult, *fbias;
+  void *out;
+  int vec_store;  // output rows and base are 16-byte aligned
+  int tiles_m, tiles_n;
+};
+
+// The operand of an instruction: 32 codes, the lower half of the register block that other formats fill.
+__device__ __forceinline__ v8i operand(v4i c) { return __builtin_shufflevector(c, c, 0, 1, 2, 3, 0, 1, 2, 3); }
+constexpr int kE2M1 = 4;  // the instruction's code for the element type
+
+template <int STEP>
+__device__ __forceinline__ v4f mfma16(v4i w, v4i x, v4f acc, int ws, int xs) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w), operand(x), acc, kE2M1, kE2M1, STEP, ws, STEP, xs);
+}
+
+template <int OUT>
+struct OutType;
+template <>
+struct OutType<CWAC_OUT_FP32> {
+  typedef float T;
+  static __device__ __forceinline__ T make(float u) { return u; }
+};
+template <>
+struct OutType<CWAC_OUT_FP16> {
+  typedef uint16_t T;
+  static __device__ __forceinline__ T make(float u) { return __builtin_bit_cast(uint16_t, (_Float16)u); }
+};
+template <>
+struct OutType<CWAC_OUT_BF16> {
+  typedef uint16_t T;
+  static __device__ __forceinline__ T make(float u) { return __builtin_bit_cast(uint16_t, (__bf16)u); }
+};
+
+// ------------------------------------------------------------------------------------------
+// Few tokens or few tiles: 16 TN channels x 16 TM tokens per workgroup, K split over its W wavefronts, each of which streams its
+// panels through a ring of D units of its own in LDS (no barrier before the sums meet).  Bound: the operands' arrival - HBM for the weights of
+// a decoding step, the round trips of a short K loop.
+// ------------------------------------------------------------------------------------------
+template <int TN, int TM, int W, int D>
+struct Mx4SplitCfg {
+  static constexpr int BN = 16 * TN, BM = 16 * TM, NT = 64 * W;
+  static constexpr int UK = kMx4Panel / 2;                  // bytes of codes of a row per unit: one panel
+  static constexpr int W_BYTES = BN * UK, CODES = (BN + BM) * UK;
+  static constexpr int SCALE_LOADS = (BN + BM + 31) / 32;   // 32 rows x 8 bytes each
+  static constexpr int UNIT = CODES + SCALE_LOADS * 256;
+  static constexpr int LPU = 2 * (TN + TM) + SCALE_LOADS;   // loads per unit; of codes: 8 rows x 128 bytes each
+  static constexpr int RING = D * UNIT;
+  static constexpr int SLAB = TN * TM * 1024;
+  static constexpr int LDS_BYTES = W * RING;
+  static_assert(SLAB <= RING && LDS_BYTES <= 160 * 1024 && D * LPU < 64, "LDS budget, 6-bit load counter");
+};
+
+// (Outside the kernel template: the host pass drops the stub of a template that passes dependent arguments to these.)
+__device__ __forceinline__ void codes_to_lds(__amdgpu_buffer_rsrc_t desc, uint8_t *dst, int offset, int k0) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(desc, CWAC_LDS_PTR(dst), 16, offset, k0, 0, 0);
+}
+__device__ __forceinline__ void scales_to_lds(const uint8_t *src, uint8_t *dst) {
+  __builtin_amdgcn_global_load_lds(CWAC_GLOBAL_PTR(src), CWAC_LDS_PTR(dst), 4, 0, 0);
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // at most N loads of this wavefront outstanding
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int TN, int TM, int W, int D, int OUT>
+__global__ __launch_bounds__(64 * W) void mx4_splitk_kernel(const Mx4Params p) {
+  using C = Mx4SplitCfg<TN, TM, W, D>;
+  using O = OutType<OUT>;
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  int tile_m, tile_n;
+  tile_of_block(blockIdx.x, p.tiles_m, p.tiles_n, tile_m, tile_n);
+  const int64_t bm0 = (int64_t)tile_m * C::BM;
+  const int bn0 = tile_n * C::BN;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, quad = lane >> 4;
+  const int rows_m = p.m - bm0 < C::BM ? (int)(p.m - bm0) : C::BM;
+  const int rows_n = p.n - bn0 < C::BN ? p.n - bn0 : C::BN;
+  // rows past the last token or channel lie behind the extent: such lanes touch no memory and bring zeros
+  const __amdgpu_buffer_rsrc_t xd = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t *>(p.x + bm0 * p.ldx), 0, (int)((int64_t)(rows_m - 1) * p.ldx + p.k / 2), 0x00020000);
+  const __amdgpu_buffer_rsrc_t wd = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t *>(p.w + (int64_t)bn0 * p.ldw), 0, (int)((int64_t)(rows_n - 1) * p.ldw + p.k / 2), 0x00020000);
+  // ---- global -> LDS: lane = (row lr, 16-byte slot pc) inside a load of 8 rows; the slot of a chunk is XORed with
+  // bits 1-3 of the row (on the global side), so that 16 lanes reading one chunk of 16 rows hit distinct banks
+  const int lr = lane >> 3, pc = lane & 7;
+  int wv[2 * TN], xv[2 * TM];
+#pragma unroll
+  for (int j = 0; j < 2 * TN; ++j) wv[j] = (j * 8 + lr) * (int)p.ldw + ((pc ^ (lr >> 1) ^ ((j & 1) << 2)) << 4);
+#pragma unroll
+  for (int j = 0; j < 2 * TM; ++j) xv[j] = (j * 8 + lr) * (int)p.ldx + ((pc ^ (lr >> 1) ^ ((j & 1) << 2)) << 4);
+  // scale bytes: four per lane, rows of the weights first; rows past the end read the last row's (their codes are zeros)
+  const uint8_t *sv[C::SCALE_LOADS];
+  int64_t sstep[C::SCALE_LOADS];
+#pragma unroll
+  for (int j = 0; j < C::SCALE_LOADS; ++j) {
+    const int row = j * 32 + (lane >> 1);
+    const bool is_w = row < C::BN;
+    const int r = is_w ? (row < rows_n ? row : rows_n - 1) : (row - C::BN < rows_m ? row - C::BN : rows_m - 1);
+    sv[j] = (is_w ? p.ws + (int64_t)(bn0 + r) * 8 : p.xs + (bm0 + r) * 8) + (lane & 1) * 4;
+    sstep[j] = is_w ? (int64_t)p.n * 8 : p.m * 8;
+  }
+  uint8_t *ring = smem + wave * C::RING;
+  auto issue = [&](int d, int unit) {
+    uint8_t *dst = ring + d * C::UNIT;
+#pragma unroll
+    for (int j = 0; j < 2 * TN; ++j) codes_to_lds(wd, dst + j * 1024, wv[j], unit * C::UK);
+#pragma unroll
+    for (int j = 0; j < 2 * TM; ++j) codes_to_lds(xd, dst + C::W_BYTES + j * 1024, xv[j], unit * C::UK);
+#pragma unroll
+    for (int j = 0; j < C::SCALE_LOADS; ++j) scales_to_lds(sv[j] + unit * sstep[j], dst + C::CODES + j * 256);
+  };
+  // ---- LDS -> operands.  Step s of a panel: lane group `quad` takes block 2 quad + s of its row.
+  const int swz = (l16 >> 1) & 7;
+  auto read = [&](int d, int s, v4i(&fw)[TN], v4i(&fx)[TM]) {
+    const uint8_t *base = ring + d * C::UNIT + l16 * C::UK + (((2 * quad + s) ^ swz) << 4);
+#pragma unroll
+    for (int a = 0; a < TN; ++a) fw[a] = *reinterpret_cast<const v4i *>(base + a * 16 * C::UK);
+#pragma unroll
+    for (int b = 0; b < TM; ++b) fx[b] = *reinterpret_cast<const v4i *>(base + C::W_BYTES + b * 16 * C::UK);
+  };
+  auto read_scales = [&](int d, int(&sw)[TN], int(&sx)[TM]) {
+    const uint8_t *base = ring + d * C::UNIT + C::CODES + l16 * 8 + 2 * quad;
+#pragma unroll
+    for (int a = 0; a < TN; ++a) sw[a] = *reinterpret_cast<const uint16_t *>(base + a * 128);
+#pragma unroll
+    for (int b = 0; b < TM; ++b) sx[b] = *reinterpret_cast<const uint16_t *>(base + (TN + b) * 128);
+  };
+  v4f acc[TN][TM];
+#pragma unroll
+  for (int a = 0; a < TN; ++a)
+#pragma unroll
+    for (int b = 0; b < TM; ++b) acc[a][b] = v4f{0, 0, 0, 0};
+  v4i fw0[TN], fx0[TM], fw1[TN], fx1[TM];
+  int sw[TN], sx[TM];
+  auto mma = [&]() {
+#pragma unroll
+    for (int a = 0; a < TN; ++a)
+#pragma unroll
+      for (int b = 0; b < TM; ++b) acc[a][b] = mfma16<0>(fw0[a], fx0[b], acc[a][b], sw[a], sx[b]);
+#pragma unroll
+    for (int a = 0; a < TN; ++a)
+#pragma unroll
+      for (int b = 0; b < TM; ++b) acc[a][b] = mfma16<1>(fw1[a], fx1[b], acc[a][b], sw[a], sx[b]);
+  };
+
+  // ---- K: a contiguous range of panels per wavefront, D in flight
+  const int units = (p.k + kMx4Panel - 1) / kMx4Panel;
+  const int mine = units / W + (wave < units % W ? 1 : 0);
+  const int first = wave * (units / W) + (wave < units % W ? wave : units % W);
+#pragma unroll
+  for (int d = 0; d < D; ++d)
+    if (d < mine) issue(d, first + d);
+  int d = 0;
+#pragma unroll 1
+  for (int i = 0; i + D < mine; ++i) {
+    wait_loads<(D - 1) * C::LPU>();
+    read(d, 0, fw0, fx0);
+    read(d, 1, fw1, fx1);
+    read_scales(d, sw, sx);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));  // lgkmcnt(0): the unit is in registers, its place is free
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    issue(d, first + i + D);
+    mma();
+    d = d + 1 == D ? 0 : d + 1;
+  }
+  // Memory operations return in order: with r units issued behind a unit, it is complete at r * LPU outstanding.
+  auto last = [&](auto tag) {  // the last D units: nothing more to issue
+    constexpr int behind = decltype(tag)::value;
+    if (behind >= D || behind >= mine) return;
+    wait_loads<(behind < D ? behind * C::LPU : 0)>();
+    read(d, 0, fw0, fx0);
+    read(d, 1, fw1, fx1);
+    read_scales(d, sw, sx);
+    mma();
+    d = d + 1 == D ? 0 : d + 1;
+  };
+  static_assert(D <= 4, "one call per slot");
+  last(std::integral_constant<int, 3>{});
+  last(std::integral_constant<int, 2>{});
+  last(std::integral_constant<int, 1>{});
+  last(std::integral_constant<int, 0>{});
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+
+  // ---- the W partial tiles meet in LDS: slot 16 q + t of a 16 x 16 tile holds channels 4 q .. 4 q + 3 of token t
+#pragma unroll
+  for (int a = 0; a < TN; ++a)
+#pragma unroll
+    for (int b = 0; b < TM; ++b) reinterpret_cast<v4f *>(ring + (a * TM + b) * 1024)[lane] = acc[a][b];
+  __syncthreads();
+  constexpr int GROUPS = C::BM * C::BN / 4;
+#pragma unroll
+  for (int g0 = 0; g0 < GROUPS; g0 += C::NT) {
+    const int g = g0 + tid;
+    if (GROUPS % C::NT != 0 && g >= GROUPS) break;
+    const int cg = g % (C::BN / 4), row = g / (C::BN / 4);
+    const int tile = (cg >> 2) * TM + (row >> 4), at = (cg & 3) * 16 + (row & 15);
+    if (row >= rows_m || 4 * cg >= rows_n) continue;
+    const uint8_t *part = smem + tile * 1024 + at * 16;
+    v4f sum = *reinterpret_cast<const v4f *>(part);
+#pragma unroll
+    for (int s = 1; s < W; ++s) sum += *reinterpret_cast<const v4f *>(part + s * C::RING);
+    const int nn = bn0 + 4 * cg;
+    typename O::T u[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int ch = nn + r < p.n ? nn + r : p.n - 1;
+      float f = sum[r];
+      if (p.mult) f = f * p.mult[ch];
+      if (p.fbias) f = f + p.fbias[ch];
+      u[r] = O::make(f);
+    }
+    typename O::T *o = static_cast<typename O::T *>(p.out) + (bm0 + row) * p.ldo + nn;
+    if (p.vec_store && nn + 3 < p.n) {
+      if constexpr (sizeof(typename O::T) == 4)
+        *reinterpret_cast<v4f *>(o) = v4f{u[0], u[1], u[2], u[3]};
+      else
+        *reinterpret_cast<uint2 *>(o) = make_uint2((uint32_t)u[0] | (uint32_t)u[1] << 16, (uint32_t)u[2] | (uint32_t)u[3] << 16);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (nn + r < p.n) o[r] = u[r];
+    }
+  }
+}
+
+template <int TN, int TM, int W, int D, int OUT>
+cwac_status launch_split_one(const Mx4Params &p, unsigned blocks, hipStream_t st) {
+  constexpr int LDS = Mx4SplitCfg<TN, TM, W, D>::LDS_BYTES;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(&mx4_splitk_kernel<TN, TM, W, D, OUT>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  if (attr != hipSuccess) return CWAC_E_LAUNCH;
+  mx4_splitk_kernel<TN, TM, W, D, OUT><<<blocks, 64 * W, LDS, st>>>(p);
+  return launch_status();
+}
+
+template <int TN, int TM, int W, int D>
+cwac_status launch_split(Mx4Params p, int out_kind, hipStream_t st) {
+  p.tiles_m = (int)ceil_div(p.m, 16 * TM);
+  p.tiles_n = (int)ceil_div(p.n, 16 * TN);
+  const int64_t blocks = (int64_t)p.tiles_m * p.tiles_n;
+  if (blocks > 0x7fffffff) return CWAC_E_SHAPE;
+  if (out_kind == CWAC_OUT_FP32) return launch_split_one<TN, TM, W, D, CWAC_OUT_FP32>(p, (unsigned)blocks, st);
+  if (out_kind == CWAC_OUT_FP16) return launch_split_one<TN, TM, W, D, CWAC_OUT_FP16>(p, (unsigned)blocks, st);
+  return launch_split_one<TN, TM, W, D, CWAC_OUT_BF16>(p, (unsigned)blocks, st);
+}
+
+}  // namespace
+}  // namespace cwac
+
+using namespace cwac;
+
+extern "C" cwac_status qlinear_mx4_cwac_forward(const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales,
+                                                const uint8_t *w_codes, int64_t ldw, const uint8_t *w_scales, int64_t m,
+                                                int32_t n, int32_t k, const float *mult, const float *fbias, int32_t out_kind,
+                                                void *out, int64_t ldo, void *stream) {
+  if (!x_codes || !x_scales || !w_codes || !w_scales || !out) return CWAC_E_NULL;
+  if (m < 1 || m > 0x7fffffff || n < 1 || k < kMx4Block || k > kMx4MaxK || k % kMx4Block != 0 || ldx < k / 2 || ldw < k / 2 ||
+      ldx > kMx4MaxPitch || ldw > kMx4MaxPitch || ldo < n)
+    return CWAC_E_SHAPE;
+  if (out_kind != CWAC_OUT_FP32 && out_kind != CWAC_OUT_FP16 && out_kind != CWAC_OUT_BF16) return CWAC_E_MODE;
+  const int64_t size = out_kind == CWAC_OUT_FP32 ? 4 : 2;
+  if (!aligned(x_codes, 16) || !aligned(w_codes, 16) || ldx % 16 != 0 || ldw % 16 != 0 || !aligned(x_scales, 8) ||
+      !aligned(w_scales, 8) || !aligned(out, (size_t)size))
+    return CWAC_E_ALIGN;
+  Mx4Params p{};
+  p.x = x_codes, p.w = w_codes, p.xs = x_scales, p.ws = w_scales;
+  p.ldx = ldx, p.ldw = ldw, p.ldo = ldo, p.m = m, p.n = n, p.k = k;
+  p.mult = mult, p.fbias = fbias, p.out = out;
+  p.vec_store = aligned(out, 16) && (ldo * size) % 16 == 0;
+  hipStream_t st = as_stream(stream);
+  if (m <= 16) return launch_split<1, 1, 4, 4>(p, out_kind, st);
+  return launch_split<2, 2, 4, 2>(p, out_kind, st);
+}

@@ -1,0 +1,191 @@
+"""Microscaled 4-bit quantizer and layer on the GPU against the 64-bit oracle."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_20932_amd as P
+from oracle import mx4_oracle as mx
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+# relative half step of a rounding to the type, and of the fp32 sum and the two fp32 epilogue operations
+EPS = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+
+
+def _strided(t, pad):
+    """The same matrix with `pad` more elements to a row."""
+    if not pad:
+        return t.contiguous()
+    full = torch.full((t.shape[0], t.shape[1] + pad), 1, dtype=t.dtype, device=t.device)
+    full[:, :t.shape[1]] = t
+    return full[:, :t.shape[1]]
+
+
+def _quantize(x, pad=0):
+    rows, k = x.shape
+    codes = torch.full((rows, k // 2 + pad), 0xEE, dtype=torch.uint8, device=DEV)[:, :k // 2]
+    scales = torch.full((-(-k // 256), rows, 8), 0xEE, dtype=torch.uint8, device=DEV)
+    P.cwac_mx4_quantize(x, codes, scales)
+    return codes, scales
+
+
+def _hard_rows(rows, k, seed):
+    """Every kind of block: ordinary, ties, zeros, subnormal, huge, saturating, negative zeros, NaN and infinities."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, k, generator=g, dtype=torch.float64)
+    x *= torch.exp2(torch.randint(-20, 10, (rows, k // 32, 1), generator=g).double()).expand(-1, -1, 32).reshape(rows, k)
+    b = x.view(rows * (k // 32), 32)
+    for i in range(0, b.shape[0], 5):
+        kind = (i // 5) % 8
+        if kind == 0:
+            b[i] = torch.randint(-28, 29, (32,), generator=g).double() / 4          # the grid's ties
+        elif kind == 1:
+            b[i] = 0.0
+        elif kind == 2:
+            b[i] *= 2.0 ** -120
+        elif kind == 3:
+            b[i] = b[i].sign() * 7.0
+        elif kind == 4:
+            b[i] = -0.0
+        elif kind == 5:
+            b[i, i % 32] = float("nan")
+        elif kind == 6:
+            b[i, (i + 7) % 32] = float("-inf")
+        else:
+            b[i] = torch.randint(-28, 29, (32,), generator=g).double() * 2.0 ** 100
+    return x
+
+
+@pytest.mark.parametrize("rows,k,pad", [(1, 32, 0), (1, 4096, 0), (3, 96, 16), (5, 544, 32), (67, 1504, 0), (130, 2048, 16),
+                                        (4099, 4128, 0), (9001, 2560, 16)])
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+def test_codes_and_scales_are_the_oracles(rows, k, pad, t):
+    x = _hard_rows(rows, k, rows + k).to(TYPES[t])
+    codes, scales = _quantize(_strided(x.to(DEV), pad), pad)
+    want, want_s = mx.quantize(x.double().numpy())
+    assert np.array_equal(scales.cpu().numpy(), mx.panels(want_s))
+    assert np.array_equal(mx.unpack(codes.cpu().numpy()), want)
+    # beyond the row: untouched
+    if pad:
+        full = codes.as_strided((rows - 1, k // 2 + pad), (k // 2 + pad, 1)) if rows > 1 else None
+        assert full is None or (full[:, k // 2:] == 0xEE).all()
+    for o in ("f32", "bf16", "f16"):
+        out = torch.empty(rows, k, dtype=TYPES[o], device=DEV)
+        P.cwac_mx4_dequantize(codes, scales, out)
+        v = torch.from_numpy(mx.values(want, want_s)).to(TYPES[o])
+        got = out.cpu()
+        assert torch.equal(got.isnan(), v.isnan())
+        assert torch.equal(got.nan_to_num(0.0, float("inf"), float("-inf")), v.nan_to_num(0.0, float("inf"), float("-inf")))
+
+
+def test_every_bfloat16_value():
+    """All finite bfloat16 numbers, each the largest of its block and beside smaller ones."""
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    x = bits[bits.isfinite()].view(-1, 1) * torch.linspace(1, 0, 32).bfloat16()
+    x = x.reshape(-1, 256)
+    codes, scales = _quantize(x.to(DEV))
+    want, want_s = mx.quantize(x.double().numpy())
+    assert np.array_equal(scales.cpu().numpy(), mx.panels(want_s))
+    assert np.array_equal(mx.unpack(codes.cpu().numpy()), want)
+
+
+def _layer(m, n, k, seed, act=None):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn(m, k, generator=g, device=DEV) * torch.exp(torch.randn(1, k, generator=g, device=DEV)) if act is None else act
+    w = torch.randn(n, k, generator=g, device=DEV) * k ** -0.5
+    mult = 1 + 0.1 * torch.randn(n, generator=g, device=DEV)
+    fb = torch.randn(n, generator=g, device=DEV)
+    return x, w, mult, fb
+
+
+def _values(codes, scales, k):
+    out = torch.empty(codes.shape[0], k, dtype=torch.float32, device=DEV)
+    P.cwac_mx4_dequantize(codes, scales, out)
+    return out.double()
+
+
+def _check(out, xv, wv, mult, fb, t):
+    """|error| <= (half a step of the type) * |y| + fp32 sums and epilogue: K products, each sum off by at most half a
+    step of the partial sum's bound sum |x w|; two more operations."""
+    y, bound = xv @ wv.t(), xv.abs() @ wv.abs().t()
+    k = xv.shape[1]
+    if mult is not None:
+        y, bound = y * mult.double(), bound * mult.double().abs()
+    if fb is not None:
+        y, bound = y + fb.double(), bound + fb.double().abs()
+    # an instruction adds its 64 or 128 products and the accumulator with one alignment, a rounding or truncation (one step,
+    # 2^-23) each: k / 64 of them, the join of up to eight partial sums and the two epilogue operations
+    steps = k / 64 + 1 + 8 + 2
+    tol = EPS[t] * y.abs() * (1 + 2.0 ** -10) + steps * 2.0 ** -23 * bound + (2.0 ** -25 if t == "f16" else 0.0)
+    err = (out.double() - y).abs()
+    assert (err <= tol).all(), (err - tol).max()
+
+
+SIZES = [(1, 1, 32), (1, 4096, 4096), (2, 17, 64), (5, 100, 96), (16, 256, 256), (17, 33, 288), (31, 1000, 5504), (64, 320, 1024),
+         (127, 129, 384), (128, 257, 2016), (255, 255, 160), (256, 256, 256), (257, 511, 544), (300, 2049, 1088),
+         (513, 768, 768), (700, 4100, 224), (1030, 1024, 4096), (2049, 640, 1312)]
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+def test_layer_matches_64_bits(m, n, k, t):
+    x, w, mult, fb = _layer(m, n, k, m + 3 * n + k)
+    xc, xs = _quantize(x, 16)
+    wc, ws = _quantize(w, 32)
+    pad = (n + k) % 3                                       # rows that are 16-byte aligned or not
+    out = torch.full((m, n + pad), 7.0, dtype=TYPES[t], device=DEV)
+    P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, mult, fb, out[:, :n])
+    assert (out[:, n:] == 7.0).all()
+    xv, wv = _values(xc, xs, k), _values(wc, ws, k)
+    _check(out[:, :n], xv, wv, mult, fb, t)
+    P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, None, None, out[:, :n])
+    _check(out[:, :n], xv, wv, None, None, t)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 64, 512), (40, 48, 320), (300, 300, 1056)])
+def test_nan_blocks_stay_in_their_rows_and_columns(m, n, k):
+    x, w, mult, fb = _layer(m, n, k, 5)
+    x[m // 2, k - 1] = float("nan")
+    w[n // 3, 0] = float("inf")
+    xc, xs = _quantize(x)
+    wc, ws = _quantize(w)
+    out = torch.empty(m, n, dtype=torch.float32, device=DEV)
+    P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, mult, fb, out)
+    nan = torch.zeros(m, n, dtype=torch.bool, device=DEV)
+    nan[m // 2], nan[:, n // 3] = True, True
+    assert torch.equal(out.isnan(), nan)
+
+
+@pytest.mark.parametrize("k", [32, 96, 224, 480])
+def test_bytes_between_rows_do_not_enter(k):
+    """K that ends inside a panel: whatever lies behind a row's codes (the largest numbers here) is left out, exactly,
+    also where the true sum is zero."""
+    m, n = 37, 50
+    x, w, _, _ = _layer(m, n, k, 9)
+    x[3] = 0.0
+    xc, xs = _quantize(x, 128)
+    wc, ws = _quantize(w, 128)
+    xc.as_strided((m - 1, k // 2 + 128), (k // 2 + 128, 1))[:, k // 2:] = 0x77
+    wc.as_strided((n - 1, k // 2 + 128), (k // 2 + 128, 1))[:, k // 2:] = 0x77
+    out = torch.empty(m, n, dtype=torch.float32, device=DEV)
+    P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, None, None, out)
+    assert (out[3] == 0).all()
+    _check(out, _values(xc, xs, k), _values(wc, ws, k), None, None, "f32")
+
+
+def test_extreme_scales():
+    """Products of the largest and smallest units meet without a spurious infinity or zero."""
+    k = 256
+    x = torch.zeros(4, k, device=DEV)
+    w = torch.zeros(3, k, device=DEV)
+    x[0, 0], w[0, 0] = 2.0 ** 100, 2.0 ** -100
+    x[1, 40], w[1, 40] = 2.0 ** -126, 2.0 ** 120
+    x[2, 80], w[2, 80] = -3 * 2.0 ** 60, 2.0 ** 60
+    xc, xs = _quantize(x)
+    wc, ws = _quantize(w)
+    out = torch.empty(4, 3, dtype=torch.float32, device=DEV)
+    P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, None, None, out)
+    want = torch.zeros(4, 3)
+    want[0, 0], want[1, 1], want[2, 2] = 1.0, 2.0 ** -6, -3 * 2.0 ** 120
+    assert torch.equal(out.cpu(), want)
