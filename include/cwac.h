@@ -498,6 +498,75 @@ cwac_status qlinear_mx4_cwac_forward(const uint8_t *x_codes, int64_t ldx, const 
                                      void *stream);
 
 /* ------------------------------------------------------------------------- */
+/* Between a language model's qkv and output layers in a decoding step:        */
+/* a paged key-value cache and the attention that reads it                     */
+/* ------------------------------------------------------------------------- */
+/* The cache of one layer is a pool of pages, a page holds `page` consecutive tokens of one request (16, 32, .. 1024):
+ *   k_cache, v_cache   device [n_pages][kv_heads][page][head_dim], contiguous, 16-byte aligned; head_dim 64, 128 or 256;
+ *                      cache_type CWAC_OUT_FP16, CWAC_OUT_BF16 or CWAC_OUT_INT8
+ *   k_scales, v_scales device fp32 [n_pages][kv_heads][page], CWAC_OUT_INT8 only (NULL is allowed otherwise): value = scale * code
+ *   table              device int32 [batch, table_cols], pitch ldt: page table[b][i] holds tokens i * page .. of request b;
+ *                      table_cols * page <= 2^31 - 65
+ *   slot               page number * page + place in the page: where a token lies, 64-bit; negative: nowhere
+ * One table and one list of slots serve the caches of all layers. */
+enum { CWAC_KV_MAX_BATCH = 8192 };
+
+/* Pages and slots for a step's new tokens, on the device, from lengths that the device holds (so a captured step goes on
+ * working as requests grow).  Request b has old_lens[b] tokens in the cache and brings new_lens[b] more (negative
+ * lengths count as 0).  The rows of a step's token batch are the requests' new tokens in order.
+ *   need = ceil((old + new) / page) - ceil(old / page) pages are taken from the top of the stack free_pages[0 .. n_free), for
+ *   the requests in order: the first page is free_pages[n_free - 1].  A request whose table row is too short for it takes none
+ *   and is not served; one whose pages are beyond the end of the stack (those of the requests before it
+ *   included) is not served either.
+ *   table        in/out: the new pages' entries are written, others left
+ *   slots        device int64 [slot_capacity]: the slot of every new token in batch order; -1 for tokens of requests not
+ *                served, for tokens of a page whose entry is negative, and for rows behind the last token
+ *   token_start  device int32 [batch + 1]: first row of each request, then the number of new tokens (at most 2^31 - 1)
+ *   seq_lens     device int32 [batch]: old + new, or old for a request not served
+ *   n_left       device int32 [1]: pages left on the stack
+ * 1 <= batch <= CWAC_KV_MAX_BATCH; n_free is taken as at most free_capacity.  The call can be repeated on the same
+ * inputs; what it writes must not overlap what it reads but for the table (CWAC_E_MODE). */
+cwac_status llm_kv_assign_pages(const int32_t *old_lens, const int32_t *new_lens, int32_t batch, int32_t page,
+                                const int32_t *free_pages, int32_t free_capacity, const int32_t *n_free, int32_t *table,
+                                int64_t ldt, int32_t table_cols, int64_t *slots, int64_t slot_capacity,
+                                int32_t *token_start, int32_t *seq_lens, int32_t *n_left, void *stream);
+
+/* New keys and values into the cache: row i of k and v goes to slot slots[i]; rows with a slot outside
+ * [0, n_pages * page) are left out.  16-bit caches take the values as they are; an 8-bit cache stores round(x / s) with
+ * s = max |x| / 127 over the head's values of the token (floored at FLT_MIN * 256: cwac_quantize_rows_sym); a token's head that
+ * holds a NaN or an infinity is stored as NaN (scale NaN, codes 0).
+ *   k, v    device [tokens, kv_heads * head_dim] of `type` (CWAC_OUT_FP16 or CWAC_OUT_BF16), pitches ldk, ldv elements (they may be columns of
+ *           the qkv layer's output); 16-byte aligned, pitches % 8 == 0; a 16-bit cache is of the same type
+ *   slots   device int64 [tokens]; a slot that is named twice holds either token's values, or a mixture
+ *   tokens >= 0 (0 is a no-op) */
+cwac_status llm_kv_append(const void *k, int64_t ldk, const void *v, int64_t ldv, int32_t type, const int64_t *slots,
+                          int64_t tokens, int32_t kv_heads, int32_t head_dim, void *k_cache, void *v_cache,
+                          int32_t cache_type, float *k_scales, float *v_scales, int32_t n_pages, int32_t page,
+                          void *stream);
+
+/* Attention of one new token per request (whose own key and value are in the cache already):
+ *   out[b, h] = softmax over t of (scale * q[b, h] . k_t) times v_t,  key head h / (q_heads / kv_heads),
+ *   t in [max(0, len - window), len) for window > 0, [0, len) for window == 0, len = lens[b] (taken as at most table_cols * page).
+ * No visible token: zeros.  Tokens of a page whose table entry is not in [0, n_pages) are left out.  Nothing that the cache
+ * holds at other places than the visible tokens' enters, NaN included.
+ *   q       device [batch, q_heads * head_dim] of `type` (CWAC_OUT_FP16 or CWAC_OUT_BF16), pitch ldq; 16-byte aligned, ldq % 8 == 0
+ *   out     device, like q, pitch ldo; 8-byte aligned, ldo % 4 == 0
+ *   a 16-bit cache is of q's type; 1 <= batch <= 65535, q_heads % kv_heads == 0, kv_heads <= 1024
+ *   workspace  device, llm_paged_attention_workspace(...) bytes, 16-byte aligned, for calls in order on one stream: it holds the parts
+ *              of split lengths between the call's two launches (calls that may overlap need one each)
+ * Logits, maximum, sum and output are accumulated in fp32, a weight meets its value as binary16 (fp16) or two bfloat16 terms.
+ * How a length is split follows from batch, heads, table_cols * page and window alone: a request's result does not depend on the
+ * other requests' lengths or contents. */
+size_t llm_paged_attention_workspace(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                     int32_t table_cols, int32_t page);
+cwac_status llm_paged_attention(const void *q, int64_t ldq, int32_t type, const void *k_cache, const void *v_cache,
+                                int32_t cache_type, const float *k_scales, const float *v_scales, int32_t n_pages,
+                                int32_t page, const int32_t *table, int64_t ldt, int32_t table_cols, const int32_t *lens,
+                                int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
+                                int32_t window, void *out, int64_t ldo, void *workspace, size_t workspace_bytes,
+                                void *stream);
+
+/* ------------------------------------------------------------------------- */
 /* Glue of a Transformer block between its W8A8 linear layers                  */
 /* ------------------------------------------------------------------------- */
 /* Per-layer compensation exists because the rest of the block is non-linear (Sec. 3.2); the

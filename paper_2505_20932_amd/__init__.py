@@ -17,7 +17,7 @@ from .binding import (  # noqa: F401
     cwac_fold_fixed_point, qlinear_cwac_forward_fixed_point,
     cwac_quantize_act_bits, cwac_quantize_rows_sym_bits,
     CWAC_MX4_BLOCK, CWAC_MX4_PANEL, CWAC_OUT_BF16, cwac_mx4_dequantize, cwac_mx4_quantize, cwac_mx4_scale_bytes,
-    qlinear_mx4_cwac_forward,
+    qlinear_mx4_cwac_forward, llm_kv_append, llm_kv_assign_pages, llm_paged_attention, llm_paged_attention_workspace,
     CWAC_OUT_FP16, CWAC_W4_GROUP, cwac_w4_quantize_groupwise, cwac_w4_packed_w_bytes, cwac_w4_pack,
     cwac_fold_weight_only, qlinear_w4a16_cwac_forward, qconv2d_cwac_forward,
     vit_residual_ln_quant, vit_gelu_table, vit_table_lookup, vit_attention_int8,

@@ -50,6 +50,7 @@ EXPORTS = (
     "qlinear_w4a16_cwac_forward_ex", "cwac_forward_kernel_for",
     "cwac_static_scratch_bytes", "cwac_calibrate_stats_static",
     "cwac_mx4_scale_bytes", "cwac_mx4_quantize", "cwac_mx4_dequantize", "qlinear_mx4_cwac_forward",
+    "llm_kv_assign_pages", "llm_kv_append", "llm_paged_attention_workspace", "llm_paged_attention",
 )
 
 
@@ -172,6 +173,11 @@ def lib() -> C.CDLL:
         sig["cwac_mx4_quantize"] = (i32, [vp, i32, i64, i64, i32, vp, i64, vp, vp])
         sig["cwac_mx4_dequantize"] = (i32, [vp, i64, vp, i64, i32, vp, i32, i64, vp])
         sig["qlinear_mx4_cwac_forward"] = (i32, [vp, i64, vp, vp, i64, vp, i64, i32, i32, vp, vp, i32, vp, i64, vp])
+        sig["llm_kv_assign_pages"] = (i32, [vp, vp, i32, i32, vp, i32, vp, vp, i64, i32, vp, i64, vp, vp, vp, vp])
+        sig["llm_kv_append"] = (i32, [vp, i64, vp, i64, i32, vp, i64, i32, i32, vp, vp, i32, vp, vp, i32, i32, vp])
+        sig["llm_paged_attention_workspace"] = (sz, [i32, i32, i32, i32, i32, i32])
+        sig["llm_paged_attention"] = (i32, [vp, i64, i32, vp, vp, i32, vp, vp, i32, i32, vp, i64, i32, vp, i32, i32, i32, i32,
+                                            f32, i32, vp, i64, vp, sz, vp])
         sig["cwac_calibrate_stats_first"] = sig["cwac_calibrate_stats"]
         sig["cwac_static_scratch_bytes"] = (sz, [])
         sig["cwac_calibrate_stats_static"] = (i32, [vp, i64, vp, i64, i64, i32, vp, vp])
@@ -601,6 +607,86 @@ def qlinear_mx4_cwac_forward(x_codes: torch.Tensor, x_scales: torch.Tensor, w_co
         assert t is None or (t.dtype == torch.float32 and t.shape == (n,) and t.is_contiguous())
     _call("qlinear_mx4_cwac_forward", dev, stream, xp, ldx, xs, wp, ldw, ws, m, n, k, _ptr(mult), _ptr(fbias),
           _KIND[out.dtype], _ptr(out), _rowmajor(out))
+
+
+# --------------------------------------------------------------------------- paged key-value cache
+def _ints(t: torch.Tensor, dtype, *shape):
+    assert t.dtype == dtype and t.shape == shape and t.is_contiguous()
+    return _ptr(t)
+
+
+def _heads(t: torch.Tensor):
+    """Rows of heads, [rows, heads, head_dim], each row's heads side by side: pointer and pitch."""
+    rows, heads, d = t.shape
+    assert (heads == 1 or t.stride(1) == d) and t.stride(2) == 1, "the heads of a row lie side by side"
+    return _ptr(t), t.stride(0) if rows > 1 else max(t.stride(0), heads * d)
+
+
+def _table(table: torch.Tensor, batch: int):
+    assert table.dtype == torch.int32 and table.shape[0] == batch
+    return _ptr(table), _rowmajor(table), table.shape[1]
+
+
+def _cache(k_cache, v_cache, k_scales, v_scales, heads: int, d: int):
+    """Pointers, type and page geometry of a layer's cache [pages, heads, page, d]."""
+    pages, h, page, dim = k_cache.shape
+    assert v_cache.shape == k_cache.shape and (h, dim) == (heads, d) and v_cache.dtype == k_cache.dtype
+    assert k_cache.is_contiguous() and v_cache.is_contiguous()
+    if k_cache.dtype == torch.int8:
+        for s in (k_scales, v_scales):
+            assert s.dtype == torch.float32 and s.shape == (pages, h, page) and s.is_contiguous()
+    return _ptr(k_cache), _ptr(v_cache), _KIND[k_cache.dtype], _ptr(k_scales), _ptr(v_scales), pages, page
+
+
+def llm_kv_assign_pages(old_lens: torch.Tensor, new_lens: torch.Tensor, page: int, free_pages: torch.Tensor,
+                        n_free: torch.Tensor, table: torch.Tensor, slots: torch.Tensor, token_start: torch.Tensor,
+                        seq_lens: torch.Tensor, n_left: torch.Tensor, stream=None):
+    """old_lens, new_lens, seq_lens int32 [batch]; free_pages int32 [capacity]; n_free, n_left int32 [1]; table int32
+    [batch, columns]; slots int64 [capacity of the token batch]; token_start int32 [batch + 1]."""
+    dev = _device_of(old_lens, new_lens, free_pages, n_free, table, slots, token_start, seq_lens, n_left)
+    batch, i4 = old_lens.numel(), torch.int32
+    tp, ldt, cols = _table(table, batch)
+    _call("llm_kv_assign_pages", dev, stream, _ints(old_lens, i4, batch), _ints(new_lens, i4, batch), batch, page,
+          _ints(free_pages, i4, free_pages.numel()), free_pages.numel(), _ints(n_free, i4, 1), tp, ldt, cols,
+          _ints(slots, torch.int64, slots.numel()), slots.numel(), _ints(token_start, i4, batch + 1),
+          _ints(seq_lens, i4, batch), _ints(n_left, i4, 1))
+
+
+def llm_kv_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                  k_scales=None, v_scales=None, stream=None):
+    """k, v float16 / bfloat16 [tokens, kv_heads, head_dim] (rows may be columns of the qkv output); slots int64 [tokens];
+    caches [pages, kv_heads, page, head_dim] of the same type, or int8 with float32 scales [pages, kv_heads, page]."""
+    dev = _device_of(k, v, slots, k_cache, v_cache, k_scales, v_scales)
+    assert k.shape == v.shape and k.dtype == v.dtype
+    tokens, heads, d = k.shape
+    kp, ldk = _heads(k)
+    vp, ldv = _heads(v)
+    kc, vc, kind, ks, vs, pages, page = _cache(k_cache, v_cache, k_scales, v_scales, heads, d)
+    _call("llm_kv_append", dev, stream, kp, ldk, vp, ldv, _KIND[k.dtype], _ints(slots, torch.int64, tokens), tokens, heads, d,
+          kc, vc, kind, ks, vs, pages, page)
+
+
+def llm_paged_attention_workspace(batch: int, q_heads: int, kv_heads: int, head_dim: int, table_cols: int, page: int) -> int:
+    return int(lib().llm_paged_attention_workspace(batch, q_heads, kv_heads, head_dim, table_cols, page))
+
+
+def llm_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scales, v_scales,
+                        table: torch.Tensor, lens: torch.Tensor, scale: float, window: int, out: torch.Tensor,
+                        workspace, stream=None):
+    """q, out float16 / bfloat16 [batch, q_heads, head_dim]; caches as in llm_kv_append (scales None for 16-bit ones);
+    table int32 [batch, columns]; lens int32 [batch]; window 0: all of a request's tokens; workspace
+    llm_paged_attention_workspace bytes."""
+    dev = _device_of(q, k_cache, v_cache, k_scales, v_scales, table, lens, out, workspace)
+    batch, heads, d = q.shape
+    kv_heads = k_cache.shape[1]
+    assert out.shape == q.shape and out.dtype == q.dtype
+    qp, ldq = _heads(q)
+    op, ldo = _heads(out)
+    tp, ldt, cols = _table(table, batch)
+    kc, vc, kind, ks, vs, pages, page = _cache(k_cache, v_cache, k_scales, v_scales, kv_heads, d)
+    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _call("llm_paged_attention", dev, stream, qp, ldq, _KIND[q.dtype], kc, vc, kind, ks, vs, pages, page, tp, ldt, cols,
+          _ints(lens, torch.int32, batch), batch, heads, kv_heads, d, scale, window, op, ldo, _ptr(workspace), nbytes)
 
 
 # --------------------------------------------------------------------------- block glue

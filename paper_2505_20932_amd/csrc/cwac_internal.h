@@ -38,6 +38,15 @@ __device__ __forceinline__ float wave_min(float v) {
   return v;
 }
 
+// Between matrix instructions and code that may branch before it reads their results: 16 wait states, as many as a 16 x 16
+// instruction (8 passes) and most of what a 32 x 32 one (16 passes) takes.  The compiler puts the waits in that such a read needs within a
+// block; behind a branch it was seen to leave them out (a result read three instructions after its matrix instruction).
+__device__ __forceinline__ void settle() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // The requantizing tail of the engine epilogue (Eq. 10 with the clip of Eq. 1):
 // round half to even, clamp in fp32 to [qmin - Z_r, qmax - Z_r], then add Z_r.
 __device__ __forceinline__ int requant_code(float u, float lo, float hi, int zr) {

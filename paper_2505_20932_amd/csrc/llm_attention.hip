@@ -1,0 +1,555 @@
+// Attention of one new token per request over a paged key-value cache:
+//   o[b, h] = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q[b, h] . k_t - max),  t over the request's visible tokens.
+//
+// Bound: HBM - every visible key and value is read once, 2 to 32 operations per byte (heads that share a key head share
+// the read).  So the kernel is a stream:
+//   * a workgroup takes one request, one key head (up to 16 query heads) and a part of the length; its four wavefronts
+//     take turns over tiles of 32 tokens, each on its own: running maximum, sum and output per wavefront, joined through LDS at the
+//     end and, where the length is split, by a second small kernel through the workspace (fixed order, no atomics);
+//   * keys and values go global -> LDS directly (no registers held while they travel), per 16 tokens one contiguous piece of a page; the
+//     buffers of keys and of values are refilled in turn, so one of the two is always in flight, and two workgroups share a
+//     compute unit;
+//   * S^T = K Q^T and O^T = V^T P^T on the matrix cores: tokens are the rows of S^T, so that a lane ends up with the weights of
+//     eight tokens of one head, which is the operand layout of the second product once its sum runs over the tokens in
+//     that order - the weights never change lanes.  The values come out of LDS transposed (the transposing reads of this device).
+//     One query head uses one of 16 columns; the matrix cores are idle otherwise;
+//   * an 8-bit cache is widened in registers (exact); the keys' scales multiply the logits, the values' scales the
+//     weights, relative to a running power of two so that small ones lose nothing.
+// Weights meet the values as binary16 (half step 2^-12 of a weight) or, for bfloat16 values, as a sum of two bfloat16 numbers (2^-17): two
+// matrix instructions instead of one, which nothing waits for.  Maximum, sum and output are fp32.
+// Tokens outside [lo, len), and those of a page whose number is not one, get weight 0, and what the cache holds there is
+// replaced by 0, NaN included.
+#include <type_traits>
+
+#include "cwac_internal.h"
+#include "llm_rules.h"
+
+namespace cwac {
+namespace {
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int v2i __attribute__((ext_vector_type(2)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+#define CWAC_LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
+#define CWAC_GLOBAL_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
+
+struct PagedParams {
+  const char *q, *k, *v;
+  const float *ks, *vs;
+  const int32_t *table, *lens;
+  char *out;
+  float *part;       // [batch * q_heads][splits][head_dim], then [batch * q_heads][splits][2]: maximum and sum
+  int64_t ldq, ldo, ldt;
+  float c;           // scale * log2(e)
+  int batch, q_heads, kv_heads, group, tiles, shift, cols, n_pages, window;
+  int splits, split_tiles;
+};
+
+// The part of a request's length that is seen, in tiles, and how many splits it takes.
+struct Span {
+  int lo, len, first, tiles, used;
+  __device__ __forceinline__ Span(const PagedParams &p, int b) {
+    const int64_t cap = (int64_t)p.cols << p.shift;
+    const int l = p.lens[b];
+    len = l < 0 ? 0 : (l > cap ? (int)cap : l);
+    lo = p.window > 0 && len > p.window ? len - p.window : 0;
+    first = lo / kPagedTile;
+    tiles = len > 0 ? (len - 1) / kPagedTile + 1 - first : 0;
+    used = (tiles + p.split_tiles - 1) / p.split_tiles;
+  }
+};
+
+template <int D, bool I8>
+struct PagedCfg {
+  static constexpr int RB = D * (I8 ? 1 : 2);      // bytes of a row
+  static constexpr int CPR = RB / 16;              // 16-byte chunks of it
+  static constexpr int LB = RB / 64;               // loads (1 KiB) of 16 rows
+  static constexpr int BLOCK = 16 * RB, TILE = 2 * BLOCK;
+  static constexpr int SCALES = I8 ? 256 : 0;
+  static constexpr int WAVE = 2 * TILE + 2 * SCALES;  // a wavefront's keys, values and their scales
+  static constexpr int LOADS = 2 * LB + (I8 ? 1 : 0);
+  static constexpr int SLAB = (D + 4) * 4;            // a head's partial output, 16 bytes apart from the next bank round
+  static constexpr int JOIN = kPagedWaves * (kPagedHeads * SLAB + kPagedHeads * 8);
+  static constexpr int LDS = kPagedWaves * WAVE > JOIN ? kPagedWaves * WAVE : JOIN;
+  // chunk c of row r lies at position c ^ swz(r): 16 rows of one chunk, and 4 x 32-byte pieces of 16 rows, hit distinct banks
+  static constexpr int PER = RB >= 256 ? 1 : 256 / RB;  // rows of a bank round
+  __host__ __device__ static constexpr int swz(int r) { return (r / PER) & (CPR < 16 ? CPR - 1 : 15); }
+};
+
+__device__ __forceinline__ void to_lds16(const char *src, char *dst) {
+  __builtin_amdgcn_global_load_lds(CWAC_GLOBAL_PTR(src), CWAC_LDS_PTR(dst), 16, 0, 0);
+}
+__device__ __forceinline__ void to_lds4(const float *src, char *dst) {
+  __builtin_amdgcn_global_load_lds(CWAC_GLOBAL_PTR(src), CWAC_LDS_PTR(dst), 4, 0, 0);
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // at most N loads of this wavefront outstanding
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void wait_lds() {  // everything read from LDS is in registers
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Eight signed bytes as matrix operands.
+template <bool BF16>
+__device__ __forceinline__ u4 widen(uint32_t a, uint32_t b) {
+  u4 r;
+  const uint32_t w[2] = {a ^ 0x80808080u, b ^ 0x80808080u};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (BF16) {
+      const float f0 = (float)(w[i] & 255u) - 128.0f, f1 = (float)((w[i] >> 8) & 255u) - 128.0f;
+      const float f2 = (float)((w[i] >> 16) & 255u) - 128.0f, f3 = (float)(w[i] >> 24) - 128.0f;
+      r[2 * i] = __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
+      r[2 * i + 1] = __builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302u);
+    } else {
+      // 0x6400 | u is the binary16 number 1024 + u
+      const h2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+      const h2 lo = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w[i], 0x04010400u)) - bias;
+      const h2 hi = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w[i], 0x04030402u)) - bias;
+      r[2 * i] = __builtin_bit_cast(uint32_t, lo);
+      r[2 * i + 1] = __builtin_bit_cast(uint32_t, hi);
+    }
+  }
+  return r;
+}
+template <bool BF16>
+__device__ __forceinline__ v4f mma(u4 a, u4 b, v4f c) {
+  if constexpr (BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+// over the four lanes that hold one head's tokens
+__device__ __forceinline__ float quad_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16, 64));
+  return fmaxf(x, __shfl_xor(x, 32, 64));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
+}
+template <bool BF16>
+__device__ __forceinline__ uint16_t narrow(float f) {
+  return BF16 ? __builtin_bit_cast(uint16_t, (__bf16)f) : __builtin_bit_cast(uint16_t, (_Float16)f);
+}
+
+template <int D, bool BF16, bool I8>
+__global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const PagedParams p) {
+  using C = PagedCfg<D, I8>;
+  constexpr int KS = D / 32, DT = D / 16;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int split = blockIdx.x, h = blockIdx.y / p.tiles, ht = blockIdx.y % p.tiles, b = blockIdx.z;
+  const Span span(p, b);
+  const int heads = p.group - ht * kPagedHeads < kPagedHeads ? p.group - ht * kPagedHeads : kPagedHeads;
+  const int head0 = h * p.group + ht * kPagedHeads;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  uint16_t *out = reinterpret_cast<uint16_t *>(p.out) + b * p.ldo + (int64_t)head0 * D;
+  if (split >= span.used) {
+    if (split == 0)  // nothing is seen
+      for (int i = tid; i < heads * (D / 4); i += 64 * kPagedWaves) reinterpret_cast<u2 *>(out)[i] = u2{0, 0};
+    return;
+  }
+  // ---- this wavefront's tiles: t0 + wave, + 4, ...
+  const int t0 = span.first + split * p.split_tiles;
+  const int nt = span.tiles - split * p.split_tiles < p.split_tiles ? span.tiles - split * p.split_tiles : p.split_tiles;
+  const int mine = (nt - wave + kPagedWaves - 1) / kPagedWaves;  // at least 0
+  char *kbuf = smem + wave * C::WAVE, *vbuf = kbuf + C::TILE, *sbuf = vbuf + C::TILE;
+
+  u4 fq[KS];
+  {
+    const char *qrow = p.q + (b * p.ldq + (int64_t)(head0 + (l16 < heads ? l16 : 0)) * D) * 2;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int dim = I8 ? 16 * (4 * (s >> 1) + quad) + 8 * (s & 1) : 8 * (4 * s + quad);
+      fq[s] = *reinterpret_cast<const u4 *>(qrow + dim * 2);
+      if (l16 >= heads) fq[s] = u4{0, 0, 0, 0};
+    }
+  }
+
+  // ---- pages: lane 2 i + a holds that of block a (16 tokens) of the wavefront's tile 32 n + i; -1: not a page, or not a token
+  int ids = -1;
+  auto fetch_ids = [&](int j) {
+    const int blk = 2 * (t0 + wave + kPagedWaves * (j + (lane >> 1))) + (lane & 1);
+    const int64_t col = (int64_t)blk >> (p.shift - 4);
+    ids = -1;
+    if (col < p.cols && (int64_t)blk * 16 < span.len) {
+      const int id = p.table[b * p.ldt + col];
+      if (id >= 0 && id < p.n_pages) ids = id;
+    }
+  };
+  // row of the cache [page, head, token] at which the 16 tokens start; a missing page's loads go to page 0
+  auto row_of = [&](int id, int blk) {
+    return (((int64_t)(id < 0 ? 0 : id) * p.kv_heads + h) << p.shift) + ((blk * 16) & ((1 << p.shift) - 1));
+  };
+  const int lr = lane / C::CPR;
+  const uint32_t voff = (uint32_t)(lr * C::RB + (((lane % C::CPR) ^ C::swz(lr)) << 4));
+  auto issue = [&](const char *cache, const float *scales, int idA, int idB, int tile, char *dst, char *sdst) {
+    const int64_t ra = row_of(idA, 2 * tile), rb = row_of(idB, 2 * tile + 1);
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      const char *src = cache + (a ? rb : ra) * C::RB;
+#pragma unroll
+      for (int i = 0; i < C::LB; ++i)  // rows (1024 / RB) i + lr: their swizzle is the XOR of the parts'
+        to_lds16(src + i * 1024 + (voff ^ (uint32_t)(C::swz(i * (1024 / C::RB)) << 4)), dst + a * C::BLOCK + i * 1024);
+    }
+    if (I8) to_lds4(scales + (lane & 16 ? rb : ra) + l16, sdst);
+  };
+
+  v4f acc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i) acc[i] = v4f{0, 0, 0, 0};
+  float m = -INFINITY, l = 0.0f;
+  int ref = -1000;  // exponent of the unit of acc (8-bit caches)
+
+  int idA = -1, idB = -1;
+  if (mine > 0) {
+    fetch_ids(0);
+    idA = __builtin_amdgcn_readlane(ids, 0);
+    idB = __builtin_amdgcn_readlane(ids, 1);
+    issue(p.k, p.ks, idA, idB, t0 + wave, kbuf, sbuf);
+    issue(p.v, p.vs, idA, idB, t0 + wave, vbuf, sbuf + C::SCALES);
+  }
+#pragma unroll 1
+  for (int j = 0; j < mine; ++j) {
+    const int tile = t0 + wave + kPagedWaves * j;
+    const bool more = j + 1 < mine;
+    const bool okA = idA >= 0, okB = idB >= 0;
+    // ---- logits
+    wait_loads<C::LOADS>();
+    u4 fk[2][KS];
+    v4f ksc[2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      const char *row = kbuf + a * C::BLOCK + l16 * C::RB;
+      if (I8) {
+        ksc[a] = *reinterpret_cast<const v4f *>(sbuf + (a * 16 + 4 * quad) * 4);
+#pragma unroll
+        for (int u = 0; u < KS / 2; ++u) fk[a][u] = *reinterpret_cast<const u4 *>(row + (((4 * u + quad) ^ C::swz(l16)) << 4));
+      } else {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) fk[a][s] = *reinterpret_cast<const u4 *>(row + (((4 * s + quad) ^ C::swz(l16)) << 4));
+      }
+    }
+    wait_lds();
+    int nextA = -1, nextB = -1;
+    if (more) {
+      if (((j + 1) & 31) == 0) fetch_ids(j + 1);
+      nextA = __builtin_amdgcn_readlane(ids, 2 * ((j + 1) & 31));
+      nextB = __builtin_amdgcn_readlane(ids, 2 * ((j + 1) & 31) + 1);
+      issue(p.k, p.ks, nextA, nextB, tile + kPagedWaves, kbuf, sbuf);
+    }
+    v4f s[2] = {v4f{0, 0, 0, 0}, v4f{0, 0, 0, 0}};
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      if (I8) {
+#pragma unroll
+        for (int u = 0; u < KS / 2; ++u) {
+          s[a] = mma<BF16>(widen<BF16>(fk[a][u][0], fk[a][u][1]), fq[2 * u], s[a]);
+          s[a] = mma<BF16>(widen<BF16>(fk[a][u][2], fk[a][u][3]), fq[2 * u + 1], s[a]);
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < KS; ++t) s[a] = mma<BF16>(fk[a][t], fq[t], s[a]);
+      }
+    }
+    settle();
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      if (I8) s[a] *= ksc[a];
+      s[a] *= p.c;
+    }
+    // ---- weights.  Element i of s[a] is token 32 tile + 16 a + 4 quad + i of head l16.
+    const bool whole = okA && okB && tile * kPagedTile >= span.lo && tile * kPagedTile + kPagedTile <= span.len;
+    uint32_t seen = 0xff;  // bit 4 a + i
+    if (!whole) {
+      seen = 0;
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = tile * kPagedTile + 16 * a + 4 * quad + i;
+          const bool ok = (a ? okB : okA) && t >= span.lo && t < span.len;
+          seen |= (ok ? 1u : 0u) << (4 * a + i);
+          s[a][i] = ok ? s[a][i] : -INFINITY;
+        }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, s[a][i]);
+    const float m_new = fmaxf(m, quad_max(top));
+    const float base = m_new == -INFINITY ? 0.0f : m_new;
+    float alpha = __builtin_amdgcn_exp2f(m - base);
+    m = m_new;
+    l *= alpha;
+    float w[8];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[4 * a + i] = __builtin_amdgcn_exp2f(s[a][i] - base);
+        l += w[4 * a + i];
+      }
+
+    // ---- values
+    if (more)
+      wait_loads<C::LOADS>();
+    else
+      wait_loads<0>();
+    u4 fv[DT];
+    v4f vsc[2];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      if (I8) {
+        // eight rows (tokens 4 quad .. + 3 of both blocks) x 16 dims: lane = row l16 / 2, half l16 % 2
+        const int r = l16 >> 1, token = (r < 4 ? 0 : 16) + 4 * quad + (r & 3);
+        const char *at = vbuf + token * C::RB + ((t ^ C::swz(token & 15)) << 4) + (l16 & 1) * 8;
+        const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i *)(at));
+        fv[t][0] = (uint32_t)x[0], fv[t][1] = (uint32_t)x[1];
+      } else {
+        // per block four rows (tokens 4 quad .. + 3) x 16 dims: lane = row l16 / 4, quarter l16 % 4
+        const int r = 4 * quad + (l16 >> 2);
+        const char *at = vbuf + r * C::RB + (((2 * t + ((l16 & 3) >> 1)) ^ C::swz(r)) << 4) + (l16 & 1) * 8;
+        const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(at));
+        const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(at + C::BLOCK));
+        const u2 xu = __builtin_bit_cast(u2, x), yu = __builtin_bit_cast(u2, y);
+        fv[t] = u4{xu[0], xu[1], yu[0], yu[1]};
+      }
+    }
+    if (I8) {
+#pragma unroll
+      for (int a = 0; a < 2; ++a) vsc[a] = *reinterpret_cast<const v4f *>(sbuf + C::SCALES + (a * 16 + 4 * quad) * 4);
+    }
+    wait_lds();
+    if (more) issue(p.v, p.vs, nextA, nextB, tile + kPagedWaves, vbuf, sbuf + C::SCALES);
+    if (!whole) {  // what lies at tokens that are not seen may be anything
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        if (I8) {
+#pragma unroll
+          for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fv[t][a] &= (seen >> (4 * a + i)) & 1 ? ~0u : ~(0xffu << (8 * i));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) fv[t][i >> 1] &= (seen >> i) & 1 ? ~0u : ~(0xffffu << (16 * (i & 1)));
+        }
+      }
+    }
+    if (I8) {
+      float big = 0x1p-126f;
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (!whole && !((seen >> (4 * a + i)) & 1)) vsc[a][i] = 0.0f;
+          big = fmaxf(big, vsc[a][i]);
+        }
+      const int e = __builtin_amdgcn_frexp_expf(quad_max(big));
+      const int unit = e > ref ? e : ref;
+      alpha = __builtin_amdgcn_ldexpf(alpha, ref - unit);
+      ref = unit;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] *= __builtin_amdgcn_ldexpf(vsc[i >> 2][i & 3], -unit);
+    }
+    u4 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint16_t a0 = narrow<BF16>(w[2 * i]), a1 = narrow<BF16>(w[2 * i + 1]);
+      hi[i] = (uint32_t)a0 | (uint32_t)a1 << 16;
+      if (BF16) {
+        const float r0 = w[2 * i] - __uint_as_float((uint32_t)a0 << 16), r1 = w[2 * i + 1] - __uint_as_float((uint32_t)a1 << 16);
+        lo[i] = (uint32_t)narrow<BF16>(r0) | (uint32_t)narrow<BF16>(r1) << 16;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const u4 val = I8 ? widen<BF16>(fv[t][0], fv[t][1]) : fv[t];
+      acc[t] *= alpha;
+      acc[t] = mma<BF16>(val, hi, acc[t]);
+      if (BF16) acc[t] = mma<BF16>(val, lo, acc[t]);
+    }
+    settle();
+    idA = nextA;
+    idB = nextB;
+  }
+
+  // ---- the wavefronts' parts meet in LDS: [wave][head][D + 4], [wave][head][2]
+  l = quad_sum(l);
+  __syncthreads();
+  float *slab = reinterpret_cast<float *>(smem);
+  float *ml = slab + kPagedWaves * kPagedHeads * (D + 4);
+  float *mine_at = slab + (wave * kPagedHeads + l16) * (D + 4) + 4 * quad;
+#pragma unroll
+  for (int t = 0; t < DT; ++t) {
+    v4f o = acc[t];
+    if (I8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_ldexpf(o[i], ref);
+    }
+    *reinterpret_cast<v4f *>(mine_at + 16 * t) = o;
+  }
+  if (quad == 0) {
+    ml[(wave * kPagedHeads + l16) * 2] = m;
+    ml[(wave * kPagedHeads + l16) * 2 + 1] = l;
+  }
+  __syncthreads();
+  for (int i = tid; i < heads * (D / 4); i += 64 * kPagedWaves) {
+    const int head = i / (D / 4), d4 = i % (D / 4) * 4;
+    float top = -INFINITY;
+#pragma unroll
+    for (int s = 0; s < kPagedWaves; ++s) top = fmaxf(top, ml[(s * kPagedHeads + head) * 2]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    v4f o = {0, 0, 0, 0};
+    float sum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < kPagedWaves; ++s) {
+      const float f = __builtin_amdgcn_exp2f(ml[(s * kPagedHeads + head) * 2] - base);
+      sum += f * ml[(s * kPagedHeads + head) * 2 + 1];
+      o += f * *reinterpret_cast<const v4f *>(slab + (s * kPagedHeads + head) * (D + 4) + d4);
+    }
+    if (span.used == 1) {
+      if (sum == 0.0f) sum = 1.0f;  // no token with a page: zeros
+      const u2 r = {(uint32_t)narrow<BF16>(o[0] / sum) | (uint32_t)narrow<BF16>(o[1] / sum) << 16,
+                    (uint32_t)narrow<BF16>(o[2] / sum) | (uint32_t)narrow<BF16>(o[3] / sum) << 16};
+      *reinterpret_cast<u2 *>(out + head * D + d4) = r;
+    } else {
+      const int64_t at = ((int64_t)b * p.q_heads + head0 + head) * p.splits + split;
+      *reinterpret_cast<v4f *>(p.part + at * D + d4) = o;
+      if (d4 == 0) {
+        float *pml = p.part + (int64_t)p.batch * p.q_heads * p.splits * D + at * 2;
+        pml[0] = top;
+        pml[1] = sum;
+      }
+    }
+  }
+}
+
+// The parts of a split length: one workgroup per request and query head.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void paged_join_kernel(const PagedParams p) {
+  constexpr int G = 256 / D;  // groups of D threads, which take turns over the splits
+  __shared__ float f_s[kPagedMaxSplits], l_s[kPagedMaxSplits], o_s[G][D];
+  const int head = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const Span span(p, b);
+  if (span.used <= 1) return;
+  const int64_t at = ((int64_t)b * p.q_heads + head) * p.splits;
+  const float *pml = p.part + (int64_t)p.batch * p.q_heads * p.splits * D + at * 2;
+  for (int s = tid; s < span.used; s += 256) {
+    f_s[s] = pml[2 * s];
+    l_s[s] = pml[2 * s + 1];
+  }
+  __syncthreads();
+  float top = -INFINITY;
+  for (int s = 0; s < span.used; ++s) top = fmaxf(top, f_s[s]);
+  const float base = top == -INFINITY ? 0.0f : top;
+  float o = 0.0f, sum = 0.0f;
+  const int d = tid % D, g = tid / D;
+  for (int s = g; s < span.used; s += G) o += __builtin_amdgcn_exp2f(f_s[s] - base) * p.part[(at + s) * D + d];
+  o_s[g][d] = o;
+  for (int s = 0; s < span.used; ++s) sum += __builtin_amdgcn_exp2f(f_s[s] - base) * l_s[s];
+  __syncthreads();
+  if (g == 0) {
+#pragma unroll
+    for (int i = 1; i < G; ++i) o += o_s[i][d];
+    if (sum == 0.0f) sum = 1.0f;
+    reinterpret_cast<uint16_t *>(p.out)[b * p.ldo + (int64_t)head * D + d] = narrow<BF16>(o / sum);
+  }
+}
+
+template <int D, bool BF16, bool I8>
+cwac_status launch_paged(const PagedParams &p, hipStream_t st) {
+  constexpr int LDS = PagedCfg<D, I8>::LDS;
+  static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attention_kernel<D, BF16, I8>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  if (attr != hipSuccess) return CWAC_E_LAUNCH;
+  paged_attention_kernel<D, BF16, I8><<<dim3(p.splits, p.kv_heads * p.tiles, p.batch), 64 * kPagedWaves, LDS, st>>>(p);
+  const cwac_status s = launch_status();
+  if (s != CWAC_OK || p.splits == 1) return s;
+  paged_join_kernel<D, BF16><<<dim3(p.q_heads, p.batch), 256, 0, st>>>(p);
+  return launch_status();
+}
+template <int D>
+cwac_status launch_width(const PagedParams &p, bool bf16, bool i8, hipStream_t st) {
+  if (bf16) return i8 ? launch_paged<D, true, true>(p, st) : launch_paged<D, true, false>(p, st);
+  return i8 ? launch_paged<D, false, true>(p, st) : launch_paged<D, false, false>(p, st);
+}
+
+bool sizes_ok(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t cols, int32_t page) {
+  if (batch < 1 || batch > 65535 || kv_heads < 1 || kv_heads > 1024 || q_heads < 1 || q_heads > 16384 || q_heads % kv_heads != 0 ||
+      (head_dim != 64 && head_dim != 128 && head_dim != 256) || cols < 1)
+    return false;
+  if (page < 16 || page > 1024 || (page & (page - 1)) != 0) return false;
+  return (int64_t)cols * page <= 0x7fffffff - 64;
+}
+
+}  // namespace
+}  // namespace cwac
+
+using namespace cwac;
+
+extern "C" size_t llm_paged_attention_workspace(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                                int32_t table_cols, int32_t page) {
+  if (!sizes_ok(batch, q_heads, kv_heads, head_dim, table_cols, page)) return 0;
+  const int s = paged_splits(batch, q_heads, kv_heads, (int64_t)table_cols * page);
+  return s == 1 ? 16 : (size_t)batch * q_heads * s * (head_dim + 2) * 4;
+}
+
+extern "C" cwac_status llm_paged_attention(const void *q, int64_t ldq, int32_t type, const void *k_cache, const void *v_cache,
+                                           int32_t cache_type, const float *k_scales, const float *v_scales, int32_t n_pages,
+                                           int32_t page, const int32_t *table, int64_t ldt, int32_t table_cols,
+                                           const int32_t *lens, int32_t batch, int32_t q_heads, int32_t kv_heads,
+                                           int32_t head_dim, float scale, int32_t window, void *out, int64_t ldo,
+                                           void *workspace, size_t workspace_bytes, void *stream) {
+  if (type != CWAC_OUT_FP16 && type != CWAC_OUT_BF16) return CWAC_E_MODE;
+  const bool int8 = cache_type == CWAC_OUT_INT8;
+  if (!int8 && cache_type != type) return CWAC_E_MODE;
+  if (!sizes_ok(batch, q_heads, kv_heads, head_dim, table_cols, page) || n_pages < 1 || window < 0 || ldt < table_cols ||
+      ldq < (int64_t)q_heads * head_dim || ldo < (int64_t)q_heads * head_dim)
+    return CWAC_E_SHAPE;
+  if (!q || !k_cache || !v_cache || !table || !lens || !out || (int8 && (!k_scales || !v_scales))) return CWAC_E_NULL;
+  if (!aligned(q, 16) || ldq % 8 != 0 || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(table, 4) || !aligned(lens, 4) ||
+      !aligned(out, 8) || ldo % 4 != 0 || (int8 && (!aligned(k_scales, 4) || !aligned(v_scales, 4))))
+    return CWAC_E_ALIGN;
+  PagedParams p{};
+  // a window's tokens lie in at most one tile more than its own number
+  int64_t tokens = (int64_t)table_cols * page;
+  if (window > 0 && window + kPagedTile - 1 < tokens) tokens = window + kPagedTile - 1;
+  p.splits = paged_splits(batch, q_heads, kv_heads, tokens);
+  const int64_t chunk = paged_chunk(tokens, p.splits);
+  p.splits = (int)ceil_div(tokens, chunk);
+  p.split_tiles = (int)(chunk / kPagedTile);
+  if (p.splits > 1) {
+    if (!workspace || workspace_bytes < (size_t)batch * q_heads * p.splits * (head_dim + 2) * 4) return CWAC_E_WORKSPACE;
+    if (!aligned(workspace, 16)) return CWAC_E_ALIGN;
+  }
+  p.q = static_cast<const char *>(q), p.k = static_cast<const char *>(k_cache), p.v = static_cast<const char *>(v_cache);
+  p.ks = k_scales, p.vs = v_scales, p.table = table, p.lens = lens, p.out = static_cast<char *>(out);
+  p.part = static_cast<float *>(workspace);
+  p.ldq = ldq, p.ldo = ldo, p.ldt = ldt, p.c = scale * 1.44269504088896340736f;
+  p.batch = batch, p.q_heads = q_heads, p.kv_heads = kv_heads, p.group = q_heads / kv_heads;
+  p.tiles = (p.group + kPagedHeads - 1) / kPagedHeads;
+  for (p.shift = 4; (1 << p.shift) < page;) ++p.shift;
+  p.cols = table_cols, p.n_pages = n_pages, p.window = window;
+  hipStream_t st = as_stream(stream);
+  if (head_dim == 64) return launch_width<64>(p, type == CWAC_OUT_BF16, int8, st);
+  if (head_dim == 128) return launch_width<128>(p, type == CWAC_OUT_BF16, int8, st);
+  return launch_width<256>(p, type == CWAC_OUT_BF16, int8, st);
+}

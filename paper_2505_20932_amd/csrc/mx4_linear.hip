@@ -219,7 +219,7 @@ __global__ __launch_bounds__(64 * W) void mx4_splitk_kernel(const Mx4Params p) {
   last(std::integral_constant<int, 1>{});
   last(std::integral_constant<int, 0>{});
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
+  settle();
 
   // ---- the W partial tiles meet in LDS: slot 16 q + t of a 16 x 16 tile holds channels 4 q .. 4 q + 3 of token t
 #pragma unroll
