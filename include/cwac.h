@@ -712,7 +712,7 @@ enum {
                                  epilogue but the fused statistics; convolutions take CWAC_SHAPE_256_8W) */
 };
 typedef struct cwac_tuning {
-  int32_t kernel;         /* CWAC_KERNEL_*: int8 linear / convolution / table / fixed-point forwards */
+  int32_t kernel;         /* CWAC_KERNEL_*: int8 linear / convolution / table / fixed-point forwards, 4-bit forward */
   int32_t shape;          /* CWAC_SHAPE_*: tile shape of the direct-to-LDS kernel for n >= 256 (used when that
                              kernel runs; k % 128 != 0 always takes CWAC_SHAPE_128_PAIR or _128_128) */
   int32_t stats_waves;    /* qlinear_cwac_calibrate_fused_ex: 0 (= 8) | 8 | 4 wavefronts per tile */
@@ -765,6 +765,12 @@ cwac_status qlinear_cwac_forward_fixed_point_ex(const int8_t *x_q, int64_t ldx, 
                                                 const int32_t *shift, const int32_t *offset,
                                                 int8_t *out, int64_t ldo, const cwac_tuning *tuning,
                                                 void *stream);
+/* kernel: CWAC_KERNEL_DIRECT_LDS the tiles (shape CWAC_SHAPE_256_8W: m, n >= 256, CWAC_SHAPE_128_128: m, n >= 128, or the larger that
+ * fits), CWAC_KERNEL_SPLIT_K the kernel that splits K over a workgroup's wavefronts; anything else the automatic choice. */
+cwac_status qlinear_mx4_cwac_forward_ex(const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales,
+                                        const uint8_t *w_codes, int64_t ldw, const uint8_t *w_scales, int64_t m, int32_t n,
+                                        int32_t k, const float *mult, const float *fbias, int32_t out_kind, void *out,
+                                        int64_t ldo, const cwac_tuning *tuning, void *stream);
 cwac_status qlinear_w4a16_cwac_forward_ex(const uint16_t *x, int64_t ldx, const void *packed_w,
                                           const uint32_t *packed_sz, int64_t m, int32_t n, int32_t k,
                                           const float *mult, const float *fbias, int32_t out_kind,

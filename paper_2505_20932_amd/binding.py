@@ -50,6 +50,7 @@ EXPORTS = (
     "qlinear_w4a16_cwac_forward_ex", "cwac_forward_kernel_for",
     "cwac_static_scratch_bytes", "cwac_calibrate_stats_static",
     "cwac_mx4_scale_bytes", "cwac_mx4_quantize", "cwac_mx4_dequantize", "qlinear_mx4_cwac_forward",
+    "qlinear_mx4_cwac_forward_ex",
     "llm_kv_assign_pages", "llm_kv_append", "llm_paged_attention_workspace", "llm_paged_attention",
 )
 
@@ -184,7 +185,7 @@ def lib() -> C.CDLL:
         sig["cwac_forward_kernel_for"] = (i32, [i64, i32, i32, i64, i64, i32, tup])
         for name in ("qlinear_cwac_forward", "qlinear_cwac_forward_table", "qconv2d_cwac_forward",
                      "qlinear_cwac_calibrate_fused", "qlinear_cwac_forward_fixed_point",
-                     "qlinear_w4a16_cwac_forward"):
+                     "qlinear_w4a16_cwac_forward", "qlinear_mx4_cwac_forward"):
             res, args = sig[name]                       # _ex: the same call with a tuning before the stream
             sig[name + "_ex"] = (res, args[:-1] + [tup, vp])
         for name, (res, args) in sig.items():
@@ -581,6 +582,8 @@ def _mx4(codes: torch.Tensor, scales: torch.Tensor, rows: int, k: int):
 
 def cwac_mx4_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None):
     """x float32 / float16 / bfloat16 [rows, k]; codes uint8 [rows, k/2]; scales uint8 [ceil(k/256), rows, 8]."""
+    if (_calls or _fast_calls()).mx4_quantize(x, codes, scales, stream):
+        return
     dev = _device_of(x, codes, scales)
     rows, k = x.shape
     cp, ldc, sp = _mx4(codes, scales, rows, k)
@@ -589,6 +592,8 @@ def cwac_mx4_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor
 
 def cwac_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, stream=None):
     """The values of the codes into out float32 / float16 / bfloat16 [rows, k]."""
+    if (_calls or _fast_calls()).mx4_dequantize(codes, scales, out, stream):
+        return
     dev = _device_of(out, codes, scales)
     rows, k = out.shape
     cp, ldc, sp = _mx4(codes, scales, rows, k)
@@ -596,17 +601,22 @@ def cwac_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Te
 
 
 def qlinear_mx4_cwac_forward(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor,
-                             w_scales: torch.Tensor, mult, fbias, out: torch.Tensor, stream=None):
+                             w_scales: torch.Tensor, mult, fbias, out: torch.Tensor, stream=None, tuning=None):
     """Codes and scales as cwac_mx4_quantize leaves them; mult, fbias float32 [n] or None; out float32 / float16 /
     bfloat16 [m, n]."""
+    if tuning is None and (_calls or _fast_calls()).mx4_forward(x_codes, x_scales, w_codes, w_scales, mult, fbias, out, stream):
+        return
     dev = _device_of(x_codes, x_scales, w_codes, w_scales, mult, fbias, out)
     (m, n), k = out.shape, 2 * x_codes.shape[1]
     xp, ldx, xs = _mx4(x_codes, x_scales, m, k)
     wp, ldw, ws = _mx4(w_codes, w_scales, n, k)
     for t in (mult, fbias):
         assert t is None or (t.dtype == torch.float32 and t.shape == (n,) and t.is_contiguous())
-    _call("qlinear_mx4_cwac_forward", dev, stream, xp, ldx, xs, wp, ldw, ws, m, n, k, _ptr(mult), _ptr(fbias),
-          _KIND[out.dtype], _ptr(out), _rowmajor(out))
+    args = (xp, ldx, xs, wp, ldw, ws, m, n, k, _ptr(mult), _ptr(fbias), _KIND[out.dtype], _ptr(out), _rowmajor(out))
+    if tuning is None:
+        _call("qlinear_mx4_cwac_forward", dev, stream, *args)
+    else:
+        _call("qlinear_mx4_cwac_forward_ex", dev, stream, *args, _tun(tuning))
 
 
 # --------------------------------------------------------------------------- paged key-value cache
@@ -643,6 +653,9 @@ def llm_kv_assign_pages(old_lens: torch.Tensor, new_lens: torch.Tensor, page: in
                         seq_lens: torch.Tensor, n_left: torch.Tensor, stream=None):
     """old_lens, new_lens, seq_lens int32 [batch]; free_pages int32 [capacity]; n_free, n_left int32 [1]; table int32
     [batch, columns]; slots int64 [capacity of the token batch]; token_start int32 [batch + 1]."""
+    if (_calls or _fast_calls()).kv_assign(old_lens, new_lens, page, free_pages, n_free, table, slots, token_start, seq_lens,
+                                           n_left, stream):
+        return
     dev = _device_of(old_lens, new_lens, free_pages, n_free, table, slots, token_start, seq_lens, n_left)
     batch, i4 = old_lens.numel(), torch.int32
     tp, ldt, cols = _table(table, batch)
@@ -656,6 +669,8 @@ def llm_kv_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_cache
                   k_scales=None, v_scales=None, stream=None):
     """k, v float16 / bfloat16 [tokens, kv_heads, head_dim] (rows may be columns of the qkv output); slots int64 [tokens];
     caches [pages, kv_heads, page, head_dim] of the same type, or int8 with float32 scales [pages, kv_heads, page]."""
+    if (_calls or _fast_calls()).kv_append(k, v, slots, k_cache, v_cache, k_scales, v_scales, stream):
+        return
     dev = _device_of(k, v, slots, k_cache, v_cache, k_scales, v_scales)
     assert k.shape == v.shape and k.dtype == v.dtype
     tokens, heads, d = k.shape
@@ -676,6 +691,9 @@ def llm_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.T
     """q, out float16 / bfloat16 [batch, q_heads, head_dim]; caches as in llm_kv_append (scales None for 16-bit ones);
     table int32 [batch, columns]; lens int32 [batch]; window 0: all of a request's tokens; workspace
     llm_paged_attention_workspace bytes."""
+    if (_calls or _fast_calls()).paged_attention(q, k_cache, v_cache, k_scales, v_scales, table, lens, scale, window, out,
+                                                 workspace, stream):
+        return
     dev = _device_of(q, k_cache, v_cache, k_scales, v_scales, table, lens, out, workspace)
     batch, heads, d = q.shape
     kv_heads = k_cache.shape[1]
@@ -799,6 +817,7 @@ qconv2d_cwac_forward_ex = _ex(qconv2d_cwac_forward)
 qlinear_cwac_calibrate_fused_ex = _ex(qlinear_cwac_calibrate_fused)
 qlinear_cwac_forward_fixed_point_ex = _ex(qlinear_cwac_forward_fixed_point)
 qlinear_w4a16_cwac_forward_ex = _ex(qlinear_w4a16_cwac_forward)
+qlinear_mx4_cwac_forward_ex = _ex(qlinear_mx4_cwac_forward)
 
 
 # --------------------------------------------------------------------------- diagnostic

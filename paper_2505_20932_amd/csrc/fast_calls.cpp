@@ -29,6 +29,12 @@ struct Entries {
   decltype(&::qlinear_cwac_forward_fixed_point) forward_fixed_point;
   decltype(&::qconv2d_cwac_forward) conv2d;
   decltype(&::qlinear_w4a16_cwac_forward) w4a16;
+  decltype(&::cwac_mx4_quantize) mx4_quantize;
+  decltype(&::cwac_mx4_dequantize) mx4_dequantize;
+  decltype(&::qlinear_mx4_cwac_forward) mx4_forward;
+  decltype(&::llm_kv_assign_pages) kv_assign;
+  decltype(&::llm_kv_append) kv_append;
+  decltype(&::llm_paged_attention) paged_attention;
 } g;
 PyObject *g_qparams_type = nullptr, *g_check = nullptr;  // the binding's structure type and its check of a status
 
@@ -312,6 +318,222 @@ PyObject *py_w4a16(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// ---- microscaled 4-bit format and paged cache: all tensors on the current device (the ctypes form serves another one)
+constexpr auto kU8 = at::kByte;
+constexpr auto kI32 = at::kInt;
+constexpr auto kI64 = at::kLong;
+
+int32_t kind_of(at::ScalarType t) {
+  return t == at::kFloat ? CWAC_OUT_FP32 : t == at::kHalf ? CWAC_OUT_FP16 : t == at::kBFloat16 ? CWAC_OUT_BF16 : t == at::kChar ? CWAC_OUT_INT8 : -1;
+}
+
+struct HereArgs : Args {
+  const c10::DeviceIndex device = c10::hip::current_device();
+  const at::TensorBase *here(PyObject *o) {
+    const at::TensorBase *t = tensor(o);
+    if (t && t->device().index() != device) ok = false;
+    return ok ? t : nullptr;
+  }
+  // contiguous, of a type, with `n` elements (-1: any number); NULL without one
+  template <typename T>
+  T *flat(PyObject *o, at::ScalarType type, int64_t n) {
+    const at::TensorBase *t = here(o);
+    if (!t || t->scalar_type() != type || !t->is_contiguous() || t->dim() != 1 || (n >= 0 && t->numel() != n)) return ok = false, nullptr;
+    return static_cast<T *>(t->data_ptr());
+  }
+  template <typename T>
+  T *flat_or_none(PyObject *o, at::ScalarType type, int64_t n) {
+    return o == Py_None ? nullptr : flat<T>(o, type, n);
+  }
+  // a matrix with contiguous rows, any type
+  const at::TensorBase *rows(PyObject *o) {
+    const at::TensorBase *t = here(o);
+    if (t && (t->dim() != 2 || t->stride(1) != 1 || t->size(1) > INT32_MAX)) ok = false;
+    return ok ? t : nullptr;
+  }
+  // codes and scales of a [rows, k] matrix in the microscaled format
+  bool mx4(PyObject *co, PyObject *so, int64_t m, int64_t k, uint8_t **codes, int64_t *ld, uint8_t **scales) {
+    const at::TensorBase *c = rows(co), *s = here(so);
+    if (!ok || c->scalar_type() != kU8 || c->size(0) != m || 2 * c->size(1) != k || s->scalar_type() != kU8 || !s->is_contiguous() ||
+        s->dim() != 3 || s->size(0) != (k + CWAC_MX4_PANEL - 1) / CWAC_MX4_PANEL || s->size(1) != m || s->size(2) != 8)
+      return ok = false;
+    *codes = static_cast<uint8_t *>(c->data_ptr());
+    *ld = pitch(*c);
+    *scales = static_cast<uint8_t *>(s->data_ptr());
+    return true;
+  }
+  // rows of heads [rows, heads, d], a row's heads side by side
+  const at::TensorBase *heads(PyObject *o, int64_t *ld) {
+    const at::TensorBase *t = here(o);
+    if (!t || t->dim() != 3 || t->stride(2) != 1 || (t->size(1) > 1 && t->stride(1) != t->size(2)) || t->size(1) > 65536 || t->size(2) > 65536)
+      return ok = false, nullptr;
+    const int64_t width = t->size(1) * t->size(2);
+    *ld = t->size(0) > 1 || t->stride(0) > width ? t->stride(0) : width;
+    return t;
+  }
+  struct Cache {
+    void *k, *v;
+    float *ks, *vs;
+    int32_t type, pages, page;
+    int64_t heads, d;
+  };
+  bool cache(PyObject *ko, PyObject *vo, PyObject *kso, PyObject *vso, Cache *c) {
+    const at::TensorBase *k = here(ko), *v = here(vo);
+    if (!ok || k->dim() != 4 || v->dim() != 4 || k->scalar_type() != v->scalar_type() || !k->is_contiguous() || !v->is_contiguous())
+      return ok = false;
+    for (int i = 0; i < 4; ++i)
+      if (k->size(i) != v->size(i) || k->size(i) > INT32_MAX) return ok = false;
+    c->k = k->data_ptr(), c->v = v->data_ptr(), c->type = kind_of(k->scalar_type());
+    c->pages = (int32_t)k->size(0), c->heads = k->size(1), c->page = (int32_t)k->size(2), c->d = k->size(3);
+    c->ks = c->vs = nullptr;
+    PyObject *so[2] = {kso, vso};
+    float **sp[2] = {&c->ks, &c->vs};
+    for (int i = 0; i < 2; ++i) {
+      if (so[i] == Py_None) continue;  // the entry point refuses an 8-bit cache without them
+      const at::TensorBase *t = here(so[i]);
+      if (!ok || c->type != CWAC_OUT_INT8 || t->scalar_type() != kF32 || !t->is_contiguous() || t->dim() != 3 || t->size(0) != c->pages ||
+          t->size(1) != c->heads || t->size(2) != c->page)
+        return ok = false;
+      *sp[i] = static_cast<float *>(t->data_ptr());
+    }
+    return true;
+  }
+};
+
+// (x, codes, scales, stream)
+PyObject *py_mx4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded("cwac_mx4_quantize", [&] {
+    HereArgs v;
+    uint8_t *c, *s;
+    int64_t ldc;
+    if (n != 4 || !g.mx4_quantize) return false;
+    const at::TensorBase *x = v.rows(a[0]);
+    if (!v.ok || kind_of(x->scalar_type()) < 0 || !v.mx4(a[1], a[2], x->size(0), x->size(1), &c, &ldc, &s)) return false;
+    void *st = v.stream(a[3]);
+    const void *xp = x->data_ptr();
+    const int32_t kind = kind_of(x->scalar_type());
+    const int64_t m = x->size(0), k = x->size(1), ldx = pitch(*x);
+    if (!v.ok) return false;
+    return unlocked([&] { return g.mx4_quantize(xp, kind, ldx, m, (int32_t)k, c, ldc, s, st); });
+  });
+}
+
+// (codes, scales, out, stream)
+PyObject *py_mx4_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded("cwac_mx4_dequantize", [&] {
+    HereArgs v;
+    uint8_t *c, *s;
+    int64_t ldc;
+    if (n != 4 || !g.mx4_dequantize) return false;
+    const at::TensorBase *o = v.rows(a[2]);
+    if (!v.ok || kind_of(o->scalar_type()) < 0 || !v.mx4(a[0], a[1], o->size(0), o->size(1), &c, &ldc, &s)) return false;
+    void *st = v.stream(a[3]), *op = o->data_ptr();
+    const int32_t kind = kind_of(o->scalar_type());
+    const int64_t m = o->size(0), k = o->size(1), ldo = pitch(*o);
+    if (!v.ok) return false;
+    return unlocked([&] { return g.mx4_dequantize(c, ldc, s, m, (int32_t)k, op, kind, ldo, st); });
+  });
+}
+
+// (x_codes, x_scales, w_codes, w_scales, mult, fbias, out, stream)
+PyObject *py_mx4_forward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded("qlinear_mx4_cwac_forward", [&] {
+    HereArgs v;
+    uint8_t *x, *xs, *w, *ws;
+    int64_t ldx, ldw;
+    if (n != 8 || !g.mx4_forward) return false;
+    const at::TensorBase *o = v.rows(a[6]), *xc = v.rows(a[0]);
+    if (!v.ok || kind_of(o->scalar_type()) < 0) return false;
+    const int64_t m = o->size(0), nn = o->size(1), k = 2 * xc->size(1), ldo = pitch(*o);
+    if (k > INT32_MAX || !v.mx4(a[0], a[1], m, k, &x, &ldx, &xs) || !v.mx4(a[2], a[3], nn, k, &w, &ldw, &ws)) return false;
+    const float *mult = v.flat_or_none<float>(a[4], kF32, nn), *fb = v.flat_or_none<float>(a[5], kF32, nn);
+    void *st = v.stream(a[7]), *op = o->data_ptr();
+    const int32_t kind = kind_of(o->scalar_type());
+    if (!v.ok) return false;
+    return unlocked([&] { return g.mx4_forward(x, ldx, xs, w, ldw, ws, m, (int32_t)nn, (int32_t)k, mult, fb, kind, op, ldo, st); });
+  });
+}
+
+// (old_lens, new_lens, page, free_pages, n_free, table, slots, token_start, seq_lens, n_left, stream)
+PyObject *py_kv_assign(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded("llm_kv_assign_pages", [&] {
+    HereArgs v;
+    if (n != 11 || !g.kv_assign) return false;
+    const at::TensorBase *old = v.here(a[0]), *fr = v.here(a[3]), *table = v.rows(a[5]), *sl = v.here(a[6]);
+    const int32_t page = (int32_t)v.integer(a[2]);
+    if (!v.ok) return false;
+    const int64_t batch = old->numel(), ldt = pitch(*table), cols = table->size(1), n_free = fr->numel(), n_slots = sl->numel();
+    if (batch > INT32_MAX - 1 || n_free > INT32_MAX || table->scalar_type() != kI32 || table->size(0) != batch) return false;
+    const int32_t *op = v.flat<int32_t>(a[0], kI32, batch), *np = v.flat<int32_t>(a[1], kI32, batch), *fp = v.flat<int32_t>(a[3], kI32, -1),
+                  *nf = v.flat<int32_t>(a[4], kI32, 1);
+    int64_t *sp = v.flat<int64_t>(a[6], kI64, -1);
+    int32_t *ts = v.flat<int32_t>(a[7], kI32, batch + 1), *sq = v.flat<int32_t>(a[8], kI32, batch), *nl = v.flat<int32_t>(a[9], kI32, 1);
+    int32_t *tp = static_cast<int32_t *>(table->data_ptr());
+    void *st = v.stream(a[10]);
+    if (!v.ok) return false;
+    return unlocked([&] {
+      return g.kv_assign(op, np, (int32_t)batch, page, fp, (int32_t)n_free, nf, tp, ldt, (int32_t)cols, sp, n_slots, ts, sq, nl, st);
+    });
+  });
+}
+
+// (k, v, slots, k_cache, v_cache, k_scales, v_scales, stream)
+PyObject *py_kv_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded("llm_kv_append", [&] {
+    HereArgs v;
+    HereArgs::Cache c;
+    int64_t ldk, ldv;
+    if (n != 8 || !g.kv_append) return false;
+    const at::TensorBase *k = v.heads(a[0], &ldk), *w = v.heads(a[1], &ldv);
+    if (!v.ok || !v.cache(a[3], a[4], a[5], a[6], &c) || k->scalar_type() != w->scalar_type()) return false;
+    const int64_t tokens = k->size(0);
+    if (w->size(0) != tokens || k->size(1) != c.heads || w->size(1) != c.heads || k->size(2) != c.d || w->size(2) != c.d) return false;
+    const int64_t *sl = v.flat<int64_t>(a[2], kI64, tokens);
+    const int32_t type = kind_of(k->scalar_type());
+    const void *kp = k->data_ptr(), *vp = w->data_ptr();
+    void *st = v.stream(a[7]);
+    if (!v.ok) return false;
+    return unlocked([&] {
+      return g.kv_append(kp, ldk, vp, ldv, type, sl, tokens, (int32_t)c.heads, (int32_t)c.d, c.k, c.v, c.type, c.ks, c.vs, c.pages, c.page, st);
+    });
+  });
+}
+
+// (q, k_cache, v_cache, k_scales, v_scales, table, lens, scale, window, out, workspace, stream)
+PyObject *py_paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded("llm_paged_attention", [&] {
+    HereArgs v;
+    HereArgs::Cache c;
+    int64_t ldq, ldo;
+    if (n != 12 || !g.paged_attention) return false;
+    const at::TensorBase *q = v.heads(a[0], &ldq), *o = v.heads(a[9], &ldo), *table = v.rows(a[5]);
+    const float scale = v.number(a[7]);
+    const int32_t window = (int32_t)v.integer(a[8]);
+    if (!v.ok || !v.cache(a[1], a[2], a[3], a[4], &c) || o->scalar_type() != q->scalar_type()) return false;
+    const int64_t batch = q->size(0), ldt = pitch(*table), cols = table->size(1);
+    for (int i = 0; i < 3; ++i)
+      if (o->size(i) != q->size(i)) return false;
+    if (batch > INT32_MAX || q->size(2) != c.d || table->scalar_type() != kI32 || table->size(0) != batch) return false;
+    const int32_t *lens = v.flat<int32_t>(a[6], kI32, batch);
+    void *ws = nullptr;
+    size_t bytes = 0;
+    if (a[10] != Py_None) {
+      const at::TensorBase *t = v.here(a[10]);
+      if (!v.ok) return false;
+      ws = t->data_ptr(), bytes = t->numel() * t->element_size();
+    }
+    const int32_t type = kind_of(q->scalar_type());
+    const int32_t *tp = static_cast<const int32_t *>(table->data_ptr());
+    const void *qp = q->data_ptr();
+    void *op = o->data_ptr(), *st = v.stream(a[11]);
+    if (!v.ok) return false;
+    return unlocked([&] {
+      return g.paged_attention(qp, ldq, type, c.k, c.v, c.type, c.ks, c.vs, c.pages, c.page, tp, ldt, (int32_t)cols, lens, (int32_t)batch,
+                               (int32_t)q->size(1), (int32_t)c.heads, (int32_t)c.d, scale, window, op, ldo, ws, bytes, st);
+    });
+  });
+}
+
 // (the type of cwac_qparams, {entry point: address}, the check of a status)
 PyObject *py_bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (n != 3 || !PyDict_Check(a[1])) return PyErr_Format(PyExc_TypeError, "bind(type, addresses, check)");
@@ -330,6 +552,20 @@ PyObject *py_bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (!v || !PyLong_Check(v)) return PyErr_Format(PyExc_KeyError, "%s", s.name);
     *s.slot = PyLong_AsVoidPtr(v);
   }
+  // these keep their address where the caller names none; without one the call is declined
+  const struct {
+    const char *name;
+    void **slot;
+  } optional[] = {{"cwac_mx4_quantize", (void **)&g.mx4_quantize},
+                  {"cwac_mx4_dequantize", (void **)&g.mx4_dequantize},
+                  {"qlinear_mx4_cwac_forward", (void **)&g.mx4_forward},
+                  {"llm_kv_assign_pages", (void **)&g.kv_assign},
+                  {"llm_kv_append", (void **)&g.kv_append},
+                  {"llm_paged_attention", (void **)&g.paged_attention}};
+  for (const auto &s : optional) {
+    PyObject *v = PyDict_GetItemString(a[1], s.name);
+    if (v && PyLong_Check(v)) *s.slot = PyLong_AsVoidPtr(v);
+  }
   Py_INCREF(a[0]);
   Py_XSETREF(g_qparams_type, a[0]);
   Py_INCREF(a[2]);
@@ -341,7 +577,9 @@ PyObject *py_bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
   { #name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr }
 PyMethodDef methods[] = {CWAC_METHOD(bind),    CWAC_METHOD(quantize_act),  CWAC_METHOD(quantize_rows_sym),
                          CWAC_METHOD(forward), CWAC_METHOD(forward_table), CWAC_METHOD(forward_fixed_point),
-                         CWAC_METHOD(conv2d),  CWAC_METHOD(w4a16),         {nullptr, nullptr, 0, nullptr}};
+                         CWAC_METHOD(conv2d),  CWAC_METHOD(w4a16),         CWAC_METHOD(mx4_quantize),
+                         CWAC_METHOD(mx4_dequantize), CWAC_METHOD(mx4_forward), CWAC_METHOD(kv_assign),
+                         CWAC_METHOD(kv_append), CWAC_METHOD(paged_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "mx4.h"
+#include "mx4_rules.h"
 #include "qlinear_common.h"
 
 namespace cwac {
@@ -37,7 +38,7 @@ struct Mx4Params {
 };
 
 // The operand of an instruction: 32 codes, the lower half of the register block that other formats fill.
-__device__ __forceinline__ v8i operand(v4i c) { return __builtin_shufflevector(c, c, 0, 1, 2, 3, 0, 1, 2, 3); }
+__device__ __forceinline__ v8i operand(v4i c) { return __builtin_shufflevector(c, c, 0, 1, 2, 3, -1, -1, -1, -1); }
 constexpr int kE2M1 = 4;  // the instruction's code for the element type
 
 template <int STEP>
@@ -83,8 +84,8 @@ struct Mx4SplitCfg {
 };
 
 // (Outside the kernel template: the host pass drops the stub of a template that passes dependent arguments to these.)
-__device__ __forceinline__ void codes_to_lds(__amdgpu_buffer_rsrc_t desc, uint8_t *dst, int offset, int k0) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(desc, CWAC_LDS_PTR(dst), 16, offset, k0, 0, 0);
+__device__ __forceinline__ void codes_to_lds(__amdgpu_buffer_rsrc_t desc, uint8_t *dst, int offset) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(desc, CWAC_LDS_PTR(dst), 16, offset, 0, 0, 0);
 }
 __device__ __forceinline__ void scales_to_lds(const uint8_t *src, uint8_t *dst) {
   __builtin_amdgcn_global_load_lds(CWAC_GLOBAL_PTR(src), CWAC_LDS_PTR(dst), 4, 0, 0);
@@ -94,6 +95,13 @@ template <int N>
 __device__ __forceinline__ void wait_loads() {  // at most N loads of this wavefront outstanding
   __builtin_amdgcn_sched_barrier(0);
   __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ void wait_lds() {  // everything read from LDS is in registers
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
@@ -140,9 +148,9 @@ __global__ __launch_bounds__(64 * W) void mx4_splitk_kernel(const Mx4Params p) {
   auto issue = [&](int d, int unit) {
     uint8_t *dst = ring + d * C::UNIT;
 #pragma unroll
-    for (int j = 0; j < 2 * TN; ++j) codes_to_lds(wd, dst + j * 1024, wv[j], unit * C::UK);
+    for (int j = 0; j < 2 * TN; ++j) codes_to_lds(wd, dst + j * 1024, wv[j] + unit * C::UK);
 #pragma unroll
-    for (int j = 0; j < 2 * TM; ++j) codes_to_lds(xd, dst + C::W_BYTES + j * 1024, xv[j], unit * C::UK);
+    for (int j = 0; j < 2 * TM; ++j) codes_to_lds(xd, dst + C::W_BYTES + j * 1024, xv[j] + unit * C::UK);
 #pragma unroll
     for (int j = 0; j < C::SCALE_LOADS; ++j) scales_to_lds(sv[j] + unit * sstep[j], dst + C::CODES + j * 256);
   };
@@ -194,10 +202,7 @@ __global__ __launch_bounds__(64 * W) void mx4_splitk_kernel(const Mx4Params p) {
     read(d, 0, fw0, fx0);
     read(d, 1, fw1, fx1);
     read_scales(d, sw, sx);
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));  // lgkmcnt(0): the unit is in registers, its place is free
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
+    wait_lds();  // the unit is in registers, its place is free
     issue(d, first + i + D);
     mma();
     d = d + 1 == D ? 0 : d + 1;
@@ -284,20 +289,302 @@ cwac_status launch_split(Mx4Params p, int out_kind, hipStream_t st) {
   return launch_split_one<TN, TM, W, D, CWAC_OUT_BF16>(p, (unsigned)blocks, st);
 }
 
+// ------------------------------------------------------------------------------------------
+// Many tiles: BM tokens x BN channels per workgroup, both panels through a ring of NSTAGE stages in LDS, one stage = one panel of 256
+// values (128 bytes of codes and 8 scale bytes per row).  Bound: the matrix cores, under the device's power limit.
+//   * Codes go global -> LDS directly, 8 rows x 128 bytes per load; the 16-byte chunk c of row r lands at position c ^ ((r >> 1) & 7)
+//     (applied on the global side), so operand reads are free of bank conflicts.  Buffer loads: what lies
+//     beyond the matrix reads as zeros, so the last panel needs no case of its own.
+//   * A stage is four steps of v_mfma_scale_f32_32x32x64: the half-wave h takes block 4 h + step of its row, so its four scale bytes
+//     are one word, read once per stage, and the instruction picks the step's byte.
+//   * Operands are double-buffered in registers: the LDS reads of a step run under the matrix instructions of the one before,
+//     those of the next stage's first step under this stage's last, behind the only barrier of the stage.
+// Tiles that reach beyond the matrix are moved inwards: their rows or channels are computed twice, with the same values.
+// ------------------------------------------------------------------------------------------
+template <int BM_, int BN_, int WM_, int TA_, int NSTAGE_>
+struct Mx4TileCfg {
+  static constexpr int BM = BM_, BN = BN_, NSTAGE = NSTAGE_, TA = TA_;  // TA: 32-channel tiles per wavefront
+  static constexpr int WM = WM_, WN = BN / (32 * TA), NW = WM * WN, NT = 64 * NW;
+  static constexpr int TB = BM / (32 * WM);                             // 32-token tiles per wavefront
+  static constexpr int BK = kMx4Panel / 2;
+  static constexpr int X_BYTES = BM * BK, W_BYTES = BN * BK, CODES = X_BYTES + W_BYTES;
+  static constexpr int STAGE = CODES + (BM + BN) * 8;                   // codes, scale bytes of the tokens, of the channels
+  static constexpr int XR = BM / NW, WR = BN / NW;                      // rows whose loads a wavefront issues
+  static constexpr int LX = XR / 8, LW = WR / 8, SX = XR / 32, SW = WR / 32, LPS = LX + LW + SX + SW;
+  static constexpr int PARAM = NSTAGE * STAGE;                          // multiplier, constant [BN]
+  static constexpr int SLAB = 32 * 272;                                 // of the epilogue: 32 rows x 256 bytes, 16 apart
+  static constexpr int LDS = PARAM + 8 * BN;
+  static_assert(XR % 32 == 0 && WR % 32 == 0 && (NSTAGE - 1) * LPS < 64 && NW * SLAB <= PARAM && LDS <= 160 * 1024, "layout");
+};
+
+template <int STEP>
+__device__ __forceinline__ v16f mfma32(v4i w, v4i x, v16f acc, int ws, int xs) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(w), operand(x), acc, kE2M1, kE2M1, STEP, ws, STEP, xs);
+}
+
+template <typename C, int OUT>
+__global__ __launch_bounds__(C::NT) void mx4_tile_kernel(const Mx4Params p) {
+  using O = OutType<OUT>;
+  constexpr int TA = C::TA, TB = C::TB, BK = C::BK, NSTAGE = C::NSTAGE;
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  float *s_mult = reinterpret_cast<float *>(smem + C::PARAM), *s_fb = s_mult + C::BN;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave_m = wave % C::WM, wave_n = wave / C::WM;
+  int tile_m, tile_n;
+  tile_of_block(blockIdx.x, p.tiles_m, p.tiles_n, tile_m, tile_n);
+  int64_t bm0 = (int64_t)tile_m * C::BM;
+  if (bm0 > p.m - C::BM) bm0 = p.m - C::BM;
+  int bn0 = tile_n * C::BN;
+  if (bn0 > p.n - C::BN) bn0 = p.n - C::BN;
+  const __amdgpu_buffer_rsrc_t xd = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t *>(p.x + bm0 * p.ldx), 0, (int)(uint32_t)((uint64_t)(C::BM - 1) * (uint64_t)p.ldx + (uint64_t)(p.k / 2)), 0x00020000);
+  const __amdgpu_buffer_rsrc_t wd = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t *>(p.w + (int64_t)bn0 * p.ldw), 0, (int)(uint32_t)((uint64_t)(C::BN - 1) * (uint64_t)p.ldw + (uint64_t)(p.k / 2)),
+      0x00020000);
+  // a lane's place in a load: row lr of 8, chunk pc ^ swizzle; loads with odd number sit 8 rows further, which flips bit 2 of
+  // the swizzle (a wavefront's rows start at a multiple of 32)
+  const int lr = lane >> 3, pc = lane & 7;
+  const uint32_t c0 = (uint32_t)((pc ^ (lr >> 1)) << 4), c1 = c0 ^ 64u;
+  const uint32_t xrow = (uint32_t)(wave * C::XR + lr) * (uint32_t)p.ldx, wrow = (uint32_t)(wave * C::WR + lr) * (uint32_t)p.ldw;
+  const uint32_t xstep = 8u * (uint32_t)p.ldx, wstep = 8u * (uint32_t)p.ldw;
+  const uint8_t *xs = p.xs + (bm0 + wave * C::XR) * 8 + lane * 4, *ws = p.ws + ((int64_t)bn0 + wave * C::WR) * 8 + lane * 4;
+  const int64_t xs_step = p.m * 8, ws_step = (int64_t)p.n * 8;
+  auto issue_x = [&](int buf, int stage) {
+    uint8_t *dst = smem + buf * C::STAGE;
+#pragma unroll
+    for (int i = 0; i < C::LX; ++i)
+      codes_to_lds(xd, dst + (wave * C::XR + 8 * i) * BK, (int)(xrow + (uint32_t)i * xstep + ((i & 1) ? c1 : c0) + (uint32_t)(stage * BK)));
+#pragma unroll
+    for (int i = 0; i < C::SX; ++i)
+      scales_to_lds(xs + stage * xs_step + i * 256, dst + C::CODES + (wave * C::XR + 32 * i) * 8);
+  };
+  auto issue_w = [&](int buf, int stage) {
+    uint8_t *dst = smem + buf * C::STAGE;
+#pragma unroll
+    for (int i = 0; i < C::LW; ++i)
+      codes_to_lds(wd, dst + C::X_BYTES + (wave * C::WR + 8 * i) * BK,
+                   (int)(wrow + (uint32_t)i * wstep + ((i & 1) ? c1 : c0) + (uint32_t)(stage * BK)));
+#pragma unroll
+    for (int i = 0; i < C::SW; ++i)
+      scales_to_lds(ws + stage * ws_step + i * 256, dst + C::CODES + (C::BM + wave * C::WR + 32 * i) * 8);
+  };
+  // ---- LDS -> operands
+  const int swz = (l32 >> 1) & 7;
+  const int x_off = (wave_m * 32 * TB + l32) * BK, w_off = C::X_BYTES + (wave_n * 32 * TA + l32) * BK;
+  const int xs_off = C::CODES + (wave_m * 32 * TB + l32) * 8 + 4 * half, ws_off = C::CODES + (C::BM + wave_n * 32 * TA + l32) * 8 + 4 * half;
+  auto read = [&](int buf, int step, v4i(&fw)[TA], v4i(&fx)[TB]) {
+    const uint8_t *base = smem + buf * C::STAGE + (((4 * half + step) ^ swz) << 4);
+#pragma unroll
+    for (int a = 0; a < TA; ++a) fw[a] = *reinterpret_cast<const v4i *>(base + w_off + a * 32 * BK);
+#pragma unroll
+    for (int b = 0; b < TB; ++b) fx[b] = *reinterpret_cast<const v4i *>(base + x_off + b * 32 * BK);
+  };
+  auto read_scales = [&](int buf, int(&sw)[TA], int(&sx)[TB]) {
+    const uint8_t *base = smem + buf * C::STAGE;
+#pragma unroll
+    for (int a = 0; a < TA; ++a) sw[a] = *reinterpret_cast<const int *>(base + ws_off + a * 256);
+#pragma unroll
+    for (int b = 0; b < TB; ++b) sx[b] = *reinterpret_cast<const int *>(base + xs_off + b * 256);
+  };
+  v16f acc[TA][TB];
+#pragma unroll
+  for (int a = 0; a < TA; ++a)
+#pragma unroll
+    for (int b = 0; b < TB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+  auto mma = [&](auto step, const v4i(&fw)[TA], const v4i(&fx)[TB], const int(&sw)[TA], const int(&sx)[TB]) {
+#pragma unroll
+    for (int a = 0; a < TA; ++a)
+#pragma unroll
+      for (int b = 0; b < TB; ++b) acc[a][b] = mfma32<decltype(step)::value>(fw[a], fx[b], acc[a][b], sw[a], sx[b]);
+  };
+  // one step for the scheduler: the LDS reads behind the first matrix instructions one by one, the loads behind the others
+  auto interleave = [&](int reads, int loads) {
+    constexpr int MM = TA * TB;
+    int r = reads, l = loads;
+#pragma unroll
+    for (int i = 0; i < MM; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      const int rn = (reads + MM - 1) / MM < 1 ? 1 : (reads + MM - 1) / MM;
+      if (r > 0) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        --r;
+        if (rn > 1 && r > 0) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          --r;
+        }
+      } else if (l > 0) {
+        __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);
+        l -= 2;
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  const int stages = (p.k + kMx4Panel - 1) / kMx4Panel;
+#pragma unroll
+  for (int s = 0; s < NSTAGE; ++s)
+    if (s < stages) {
+      issue_x(s, s);
+      issue_w(s, s);
+    }
+  for (int i = tid; i < C::BN; i += C::NT) {
+    s_mult[i] = p.mult ? p.mult[bn0 + i] : 1.0f;
+    s_fb[i] = p.fbias ? p.fbias[bn0 + i] : 0.0f;
+  }
+  if (stages >= NSTAGE)
+    wait_loads<(NSTAGE - 1) * C::LPS>();  // (the parameter loads are younger, and waited for by their stores)
+  else
+    wait_loads<0>();
+  __builtin_amdgcn_s_barrier();
+  v4i fwA[TA], fxA[TB], fwB[TA], fxB[TB];
+  int sw[TA], sx[TB];
+  read(0, 0, fwA, fxA);
+  read_scales(0, sw, sx);
+  using S0 = std::integral_constant<int, 0>;
+  using S1 = std::integral_constant<int, 1>;
+  using S2 = std::integral_constant<int, 2>;
+  using S3 = std::integral_constant<int, 3>;
+  // Stage s in ring place buf.  The loads of stage s + NSTAGE go into the place that this stage leaves, behind its barrier: the
+  // tokens' under the last step, the channels' under the first step of the next stage.
+  auto stage_body = [&](int s, int buf, auto steady) {
+    constexpr bool STEADY = decltype(steady)::value;
+    const bool late = STEADY || (s >= 1 && s - 1 + NSTAGE < stages);
+    const int prev = buf == 0 ? NSTAGE - 1 : buf - 1, next = buf == NSTAGE - 1 ? 0 : buf + 1;
+    if (late) issue_w(prev, s - 1 + NSTAGE);
+    read(buf, 1, fwB, fxB);
+    mma(S0{}, fwA, fxA, sw, sx);
+    interleave(TA + TB, late ? C::LW + C::SW : 0);
+    read(buf, 2, fwA, fxA);
+    mma(S1{}, fwB, fxB, sw, sx);
+    interleave(TA + TB, 0);
+    read(buf, 3, fwB, fxB);
+    mma(S2{}, fwA, fxA, sw, sx);
+    interleave(TA + TB, 0);
+    // stage s + 1 has landed: with NSTAGE > 2 the stages behind it may still travel
+    if (NSTAGE > 2 && (STEADY || s + NSTAGE - 1 < stages))
+      wait_loads<(NSTAGE - 2) * C::LPS>();
+    else
+      wait_loads<0>();
+    wait_lds();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    const bool first = STEADY || s + NSTAGE < stages;
+    if (first) issue_x(buf, s + NSTAGE);
+    int nw[TA], nx[TB];
+    if (STEADY || s + 1 < stages) {
+      read(next, 0, fwA, fxA);
+      read_scales(next, nw, nx);
+    }
+    mma(S3{}, fwB, fxB, sw, sx);
+    interleave(2 * (TA + TB), first ? C::LX + C::SX : 0);
+    if (STEADY || s + 1 < stages) {
+#pragma unroll
+      for (int a = 0; a < TA; ++a) sw[a] = nw[a];
+#pragma unroll
+      for (int b = 0; b < TB; ++b) sx[b] = nx[b];
+    }
+  };
+  stage_body(0, 0, std::false_type{});
+  int s = 1;
+  // steady state, unrolled over the ring so that its places are compile-time constants
+  for (; s % NSTAGE != 0 && s + NSTAGE < stages; ++s) stage_body(s, s % NSTAGE, std::true_type{});
+  for (; s + 2 * NSTAGE <= stages; s += NSTAGE) {
+#pragma unroll
+    for (int j = 0; j < NSTAGE; ++j) stage_body(s + j, j, std::true_type{});
+  }
+  for (; s < stages; ++s) stage_body(s, s % NSTAGE, std::false_type{});
+  settle();
+  settle();
+  __syncthreads();  // the slabs lie over the ring, in which a late reader may still be
+
+  // ---- epilogue.  Element 4 g + r of acc[a][b]: channel 32 a + 8 g + 4 half + r, token 32 b + l32 of the wavefront's tile.
+  // A slab is 32 tokens x 256 bytes: the channels of 2 (4-byte outputs) or 4 of the 32-channel tiles.
+  constexpr int ES = sizeof(typename O::T), AP = ES == 4 ? (TA < 2 ? TA : 2) : TA, ROW = AP * 32 * ES;
+  uint8_t *slab = smem + wave * C::SLAB;
+#pragma unroll
+  for (int b = 0; b < TB; ++b)
+#pragma unroll
+    for (int a0 = 0; a0 < TA; a0 += AP) {
+#pragma unroll
+      for (int a = a0; a < a0 + AP; ++a)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int ch = wave_n * 32 * TA + a * 32 + 8 * g + 4 * half;
+          const v4f mu = *reinterpret_cast<const v4f *>(s_mult + ch), fb = *reinterpret_cast<const v4f *>(s_fb + ch);
+          typename O::T u[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float f = acc[a][b][4 * g + r] * mu[r];
+            if (p.fbias) f = f + fb[r];
+            u[r] = O::make(f);
+          }
+          uint8_t *at = slab + l32 * 272 + ((a - a0) * 32 + 8 * g + 4 * half) * ES;
+          if constexpr (ES == 4)
+            *reinterpret_cast<v4f *>(at) = v4f{u[0], u[1], u[2], u[3]};
+          else
+            *reinterpret_cast<uint2 *>(at) = make_uint2((uint32_t)u[0] | (uint32_t)u[1] << 16, (uint32_t)u[2] | (uint32_t)u[3] << 16);
+        }
+      // (a wavefront's own slab: its LDS operations are in order)
+      typename O::T *o = static_cast<typename O::T *>(p.out) + (bm0 + wave_m * 32 * TB + 32 * b) * p.ldo + bn0 + wave_n * 32 * TA + 32 * a0;
+      if (p.vec_store && ((bn0 * ES) & 15) == 0) {
+        constexpr int LPR = ROW / 16, RPS = 64 / LPR;  // lanes per row, rows per store
+#pragma unroll
+        for (int i = 0; i < 32 / RPS; ++i) {
+          const int row = i * RPS + lane / LPR;
+          *reinterpret_cast<v4i *>(o + row * p.ldo + (lane % LPR) * (16 / ES)) =
+              *reinterpret_cast<const v4i *>(slab + row * 272 + (lane % LPR) * 16);
+        }
+      } else {
+        constexpr int EPR = ROW / ES, RPS = EPR >= 64 ? 1 : 64 / EPR;  // elements per row; whole wavefronts over consecutive ones
+        for (int row = lane / (64 / RPS); row < 32; row += RPS)
+#pragma unroll
+          for (int c = lane % (64 / RPS); c < EPR; c += 64 / RPS)
+            o[row * p.ldo + c] = *reinterpret_cast<const typename O::T *>(slab + row * 272 + c * ES);
+      }
+    }
+}
+
+template <typename C, int OUT>
+cwac_status launch_tile_one(const Mx4Params &p, unsigned blocks, hipStream_t st) {
+  static const hipError_t attr =
+      hipFuncSetAttribute(reinterpret_cast<const void *>(&mx4_tile_kernel<C, OUT>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+  if (attr != hipSuccess) return CWAC_E_LAUNCH;
+  mx4_tile_kernel<C, OUT><<<blocks, C::NT, C::LDS, st>>>(p);
+  return launch_status();
+}
+
+template <typename C>
+cwac_status launch_tile(Mx4Params p, int out_kind, hipStream_t st) {
+  p.tiles_m = (int)ceil_div(p.m, C::BM);
+  p.tiles_n = (int)ceil_div(p.n, C::BN);
+  const int64_t blocks = (int64_t)p.tiles_m * p.tiles_n;
+  if (blocks > 0x7fffffff) return CWAC_E_SHAPE;
+  if (out_kind == CWAC_OUT_FP32) return launch_tile_one<C, CWAC_OUT_FP32>(p, (unsigned)blocks, st);
+  if (out_kind == CWAC_OUT_FP16) return launch_tile_one<C, CWAC_OUT_FP16>(p, (unsigned)blocks, st);
+  return launch_tile_one<C, CWAC_OUT_BF16>(p, (unsigned)blocks, st);
+}
+
+using Tile256 = Mx4TileCfg<256, 256, 4, 4, 2>;
+using Tile128 = Mx4TileCfg<128, 128, 2, 2, 2>;
+
 }  // namespace
 }  // namespace cwac
 
 using namespace cwac;
 
-extern "C" cwac_status qlinear_mx4_cwac_forward(const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales,
-                                                const uint8_t *w_codes, int64_t ldw, const uint8_t *w_scales, int64_t m,
-                                                int32_t n, int32_t k, const float *mult, const float *fbias, int32_t out_kind,
-                                                void *out, int64_t ldo, void *stream) {
+extern "C" cwac_status qlinear_mx4_cwac_forward_ex(const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales,
+                                                   const uint8_t *w_codes, int64_t ldw, const uint8_t *w_scales, int64_t m,
+                                                   int32_t n, int32_t k, const float *mult, const float *fbias, int32_t out_kind,
+                                                   void *out, int64_t ldo, const cwac_tuning *tuning, void *stream) {
   if (!x_codes || !x_scales || !w_codes || !w_scales || !out) return CWAC_E_NULL;
   if (m < 1 || m > 0x7fffffff || n < 1 || k < kMx4Block || k > kMx4MaxK || k % kMx4Block != 0 || ldx < k / 2 || ldw < k / 2 ||
       ldx > kMx4MaxPitch || ldw > kMx4MaxPitch || ldo < n)
     return CWAC_E_SHAPE;
-  if (out_kind != CWAC_OUT_FP32 && out_kind != CWAC_OUT_FP16 && out_kind != CWAC_OUT_BF16) return CWAC_E_MODE;
+  Tune tune;
+  if ((out_kind != CWAC_OUT_FP32 && out_kind != CWAC_OUT_FP16 && out_kind != CWAC_OUT_BF16) || !tune_from(tuning, tune)) return CWAC_E_MODE;
   const int64_t size = out_kind == CWAC_OUT_FP32 ? 4 : 2;
   if (!aligned(x_codes, 16) || !aligned(w_codes, 16) || ldx % 16 != 0 || ldw % 16 != 0 || !aligned(x_scales, 8) ||
       !aligned(w_scales, 8) || !aligned(out, (size_t)size))
@@ -308,6 +595,23 @@ extern "C" cwac_status qlinear_mx4_cwac_forward(const uint8_t *x_codes, int64_t 
   p.mult = mult, p.fbias = fbias, p.out = out;
   p.vec_store = aligned(out, 16) && (ldo * size) % 16 == 0;
   hipStream_t st = as_stream(stream);
-  if (m <= 16) return launch_split<1, 1, 4, 4>(p, out_kind, st);
-  return launch_split<2, 2, 4, 2>(p, out_kind, st);
+  int form = mx4_form(m, n, k);
+  if (tune.kernel == CWAC_KERNEL_SPLIT_K) form = mx4_split_form(m, n, k);
+  if (tune.kernel == CWAC_KERNEL_DIRECT_LDS) {
+    if (m >= 128 && n >= 128 && (tune.shape == CWAC_SHAPE_128_128 || (tune.shape == CWAC_SHAPE_AUTO && (m < 256 || n < 256)))) form = kMx4Tile128;
+    if (m >= 256 && n >= 256 && (tune.shape == CWAC_SHAPE_256_8W || tune.shape == CWAC_SHAPE_AUTO)) form = kMx4Tile256;
+  }
+  switch (form) {
+    case kMx4Tile256: return launch_tile<Tile256>(p, out_kind, st);
+    case kMx4Tile128: return launch_tile<Tile128>(p, out_kind, st);
+    case kMx4Split16: return launch_split<1, 1, 4, 4>(p, out_kind, st);
+    default: return launch_split<2, 2, 4, 2>(p, out_kind, st);
+  }
+}
+
+extern "C" cwac_status qlinear_mx4_cwac_forward(const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales,
+                                                const uint8_t *w_codes, int64_t ldw, const uint8_t *w_scales, int64_t m,
+                                                int32_t n, int32_t k, const float *mult, const float *fbias, int32_t out_kind,
+                                                void *out, int64_t ldo, void *stream) {
+  return qlinear_mx4_cwac_forward_ex(x_codes, ldx, x_scales, w_codes, ldw, w_scales, m, n, k, mult, fbias, out_kind, out, ldo, nullptr, stream);
 }

@@ -122,6 +122,10 @@ def _check(out, xv, wv, mult, fb, t):
     assert (err <= tol).all(), (err - tol).max()
 
 
+B = P.binding
+# the automatic choice, each tile where it fits, the split-K kernel
+FORMS = [None, B.make_tuning(kernel=B.CWAC_KERNEL_SPLIT_K), B.make_tuning(kernel=B.CWAC_KERNEL_DIRECT_LDS, shape=B.CWAC_SHAPE_128_128),
+         B.make_tuning(kernel=B.CWAC_KERNEL_DIRECT_LDS, shape=B.CWAC_SHAPE_256_8W)]
 SIZES = [(1, 1, 32), (1, 4096, 4096), (2, 17, 64), (5, 100, 96), (16, 256, 256), (17, 33, 288), (31, 1000, 5504), (64, 320, 1024),
          (127, 129, 384), (128, 257, 2016), (255, 255, 160), (256, 256, 256), (257, 511, 544), (300, 2049, 1088),
          (513, 768, 768), (700, 4100, 224), (1030, 1024, 4096), (2049, 640, 1312)]
@@ -133,14 +137,15 @@ def test_layer_matches_64_bits(m, n, k, t):
     x, w, mult, fb = _layer(m, n, k, m + 3 * n + k)
     xc, xs = _quantize(x, 16)
     wc, ws = _quantize(w, 32)
-    pad = (n + k) % 3                                       # rows that are 16-byte aligned or not
-    out = torch.full((m, n + pad), 7.0, dtype=TYPES[t], device=DEV)
-    P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, mult, fb, out[:, :n])
-    assert (out[:, n:] == 7.0).all()
     xv, wv = _values(xc, xs, k), _values(wc, ws, k)
-    _check(out[:, :n], xv, wv, mult, fb, t)
-    P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, None, None, out[:, :n])
-    _check(out[:, :n], xv, wv, None, None, t)
+    for tuning in FORMS:
+        for pad in (0, 5, 16 + -n % 16):                    # rows that are 16-byte aligned or not
+            out = torch.full((m, n + pad), 7.0, dtype=TYPES[t], device=DEV)
+            P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, mult, fb, out[:, :n], tuning=tuning)
+            assert (out[:, n:] == 7.0).all()
+            _check(out[:, :n], xv, wv, mult, fb, t)
+        P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, None, None, out[:, :n], tuning=tuning)
+        _check(out[:, :n], xv, wv, None, None, t)
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 64, 512), (40, 48, 320), (300, 300, 1056)])
@@ -150,28 +155,30 @@ def test_nan_blocks_stay_in_their_rows_and_columns(m, n, k):
     w[n // 3, 0] = float("inf")
     xc, xs = _quantize(x)
     wc, ws = _quantize(w)
-    out = torch.empty(m, n, dtype=torch.float32, device=DEV)
-    P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, mult, fb, out)
     nan = torch.zeros(m, n, dtype=torch.bool, device=DEV)
     nan[m // 2], nan[:, n // 3] = True, True
-    assert torch.equal(out.isnan(), nan)
+    for tuning in FORMS:
+        out = torch.empty(m, n, dtype=torch.float32, device=DEV)
+        P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, mult, fb, out, tuning=tuning)
+        assert torch.equal(out.isnan(), nan)
 
 
-@pytest.mark.parametrize("k", [32, 96, 224, 480])
-def test_bytes_between_rows_do_not_enter(k):
+@pytest.mark.parametrize("m,n", [(37, 50), (140, 133), (259, 300)])
+@pytest.mark.parametrize("k", [32, 96, 224, 480, 1760])
+def test_bytes_between_rows_do_not_enter(m, n, k):
     """K that ends inside a panel: whatever lies behind a row's codes (the largest numbers here) is left out, exactly,
     also where the true sum is zero."""
-    m, n = 37, 50
     x, w, _, _ = _layer(m, n, k, 9)
     x[3] = 0.0
     xc, xs = _quantize(x, 128)
     wc, ws = _quantize(w, 128)
     xc.as_strided((m - 1, k // 2 + 128), (k // 2 + 128, 1))[:, k // 2:] = 0x77
     wc.as_strided((n - 1, k // 2 + 128), (k // 2 + 128, 1))[:, k // 2:] = 0x77
-    out = torch.empty(m, n, dtype=torch.float32, device=DEV)
-    P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, None, None, out)
-    assert (out[3] == 0).all()
-    _check(out, _values(xc, xs, k), _values(wc, ws, k), None, None, "f32")
+    for tuning in FORMS:
+        out = torch.empty(m, n, dtype=torch.float32, device=DEV)
+        P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, None, None, out, tuning=tuning)
+        assert (out[3] == 0).all()
+        _check(out, _values(xc, xs, k), _values(wc, ws, k), None, None, "f32")
 
 
 def test_extreme_scales():

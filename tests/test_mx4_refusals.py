@@ -71,3 +71,10 @@ def test_layer(lib):
     for bad in (dict(x=ODD8), dict(w=ODD8), dict(ldx=72), dict(ldw=72), dict(xs=ODD4), dict(ws=ODD4), dict(out=C.c_void_p(4098))):
         assert call(**bad) == -3, bad
     assert call(kind=F16, out=C.c_void_p(4097)) == -3
+
+
+def test_tuning(lib):
+    f = lib.qlinear_mx4_cwac_forward_ex
+    for bad in (binding.make_tuning(kernel=7), binding.make_tuning(shape=9), binding.make_tuning(persist_loaders=3)):
+        assert f(A, 64, A, A, 64, A, 4, 4, 128, NULL, NULL, F32, A, 4, C.byref(bad), NULL) == -4
+    assert f(A, 64, A, A, 64, A, 4, 4, 144, NULL, NULL, F32, A, 4, C.byref(binding.make_tuning()), NULL) == -2
