@@ -554,7 +554,7 @@ cwac_status llm_kv_append(const void *k, int64_t ldk, const void *v, int64_t ldv
  *   a 16-bit cache is of q's type; 1 <= batch <= 65535, q_heads % kv_heads == 0, kv_heads <= 1024
  *   workspace  device, llm_paged_attention_workspace(...) bytes, 16-byte aligned, for calls in order on one stream: it holds the parts
  *              of split lengths between the call's two launches (calls that may overlap need one each)
- * Logits, maximum, sum and output are accumulated in fp32, a weight meets its value as binary16 (fp16) or two bfloat16 terms.
+ * Logits, maximum, sum and output are accumulated in fp32, a weight meets its value as the sum of two terms of `type`.
  * How a length is split follows from batch, heads, table_cols * page and window alone: a request's result does not depend on the
  * other requests' lengths or contents. */
 size_t llm_paged_attention_workspace(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim,

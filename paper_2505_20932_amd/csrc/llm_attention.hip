@@ -13,10 +13,12 @@
 //     eight tokens of one head, which is the operand layout of the second product once its sum runs over the tokens in
 //     that order - the weights never change lanes.  The values come out of LDS transposed (the transposing reads of this device).
 //     One query head uses one of 16 columns; the matrix cores are idle otherwise;
-//   * an 8-bit cache is widened in registers (exact); the keys' scales multiply the logits, the values' scales the
-//     weights, relative to a running power of two so that small ones lose nothing.
-// Weights meet the values as binary16 (half step 2^-12 of a weight) or, for bfloat16 values, as a sum of two bfloat16 numbers (2^-17): two
-// matrix instructions instead of one, which nothing waits for.  Maximum, sum and output are fp32.
+//   * an 8-bit cache is widened to binary16 in registers (exact); the keys' scales multiply the logits, the values' scales the
+//     weights, relative to a running power of two so that small ones lose nothing.  bfloat16 queries become binary16 relative to
+//     the head's largest one (what falls below 2^-25 of that is lost).
+// Over 16-bit caches weights meet the values as a sum of two numbers of the values' type (rounded at 2^-22 or 2^-17 of a weight): two
+// matrix instructions instead of one, which nothing waits for.  Over 8-bit caches, where the vector ALU sets the pace, as one
+// binary16 number (2^-12).  Maximum, sum and output are fp32.
 // Tokens outside [lo, len), and those of a page whose number is not one, get weight 0, and what the cache holds there is
 // replaced by 0, NaN included.
 #include <type_traits>
@@ -47,7 +49,8 @@ struct PagedParams {
   char *out;
   float *part;       // [batch * q_heads][splits][head_dim], then [batch * q_heads][splits][2]: maximum and sum
   int64_t ldq, ldo, ldt;
-  float c;           // scale * log2(e)
+  float c;           // |scale| * log2(e), at least 2^-126
+  int negate;        // scale < 0: the queries change sign
   int batch, q_heads, kv_heads, group, tiles, shift, cols, n_pages, window;
   int splits, split_tiles;
 };
@@ -83,8 +86,8 @@ struct PagedCfg {
   __host__ __device__ static constexpr int swz(int r) { return (r / PER) & (CPR < 16 ? CPR - 1 : 15); }
 };
 
-__device__ __forceinline__ void to_lds16(const char *src, char *dst) {
-  __builtin_amdgcn_global_load_lds(CWAC_GLOBAL_PTR(src), CWAC_LDS_PTR(dst), 16, 0, 0);
+__device__ __forceinline__ void to_lds16(const char *src, uint32_t offset, char *dst) {
+  __builtin_amdgcn_global_load_lds(CWAC_GLOBAL_PTR(src + offset), CWAC_LDS_PTR(dst), 16, 0, 0);
 }
 __device__ __forceinline__ void to_lds4(const float *src, char *dst) {
   __builtin_amdgcn_global_load_lds(CWAC_GLOBAL_PTR(src), CWAC_LDS_PTR(dst), 4, 0, 0);
@@ -103,26 +106,17 @@ __device__ __forceinline__ void wait_lds() {  // everything read from LDS is in 
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Eight signed bytes as matrix operands.
-template <bool BF16>
+// Eight signed bytes as binary16 numbers: 0x6400 | u is 1024 + u for a byte u = code + 128.
 __device__ __forceinline__ u4 widen(uint32_t a, uint32_t b) {
   u4 r;
   const uint32_t w[2] = {a ^ 0x80808080u, b ^ 0x80808080u};
+  const h2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    if (BF16) {
-      const float f0 = (float)(w[i] & 255u) - 128.0f, f1 = (float)((w[i] >> 8) & 255u) - 128.0f;
-      const float f2 = (float)((w[i] >> 16) & 255u) - 128.0f, f3 = (float)(w[i] >> 24) - 128.0f;
-      r[2 * i] = __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
-      r[2 * i + 1] = __builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302u);
-    } else {
-      // 0x6400 | u is the binary16 number 1024 + u
-      const h2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
-      const h2 lo = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w[i], 0x04010400u)) - bias;
-      const h2 hi = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w[i], 0x04030402u)) - bias;
-      r[2 * i] = __builtin_bit_cast(uint32_t, lo);
-      r[2 * i + 1] = __builtin_bit_cast(uint32_t, hi);
-    }
+    const h2 lo = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w[i], 0x04010400u)) - bias;
+    const h2 hi = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w[i], 0x04030402u)) - bias;
+    r[2 * i] = __builtin_bit_cast(uint32_t, lo);
+    r[2 * i + 1] = __builtin_bit_cast(uint32_t, hi);
   }
   return r;
 }
@@ -133,31 +127,85 @@ __device__ __forceinline__ v4f mma(u4 a, u4 b, v4f c) {
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
 }
-// over the four lanes that hold one head's tokens
+// Over the four lanes l16, l16 + 16, + 32, + 48 that hold one head's tokens: the register swaps hand every lane its
+// own value and its partner's.
+template <typename F>
+__device__ __forceinline__ float over_quads(float x, F op) {
+  const uint32_t a = __float_as_uint(x);
+  const auto p = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  const uint32_t b = __float_as_uint(op(__uint_as_float(p[0]), __uint_as_float(p[1])));
+  const auto q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return op(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
 __device__ __forceinline__ float quad_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16, 64));
-  return fmaxf(x, __shfl_xor(x, 32, 64));
+  return over_quads(x, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float quad_sum(float x) {
-  x += __shfl_xor(x, 16, 64);
-  return x + __shfl_xor(x, 32, 64);
+  return over_quads(x, [](float a, float b) { return a + b; });
+}
+// Transposing reads of the values, written out because the compiler puts a wait for ALL loads in flight before the builtin; the wait
+// for the reads themselves is part of the block.  `at`: LDS byte address of a lane's piece, `second`: of the other block of 16 tokens.
+template <int SECOND>
+__device__ __forceinline__ void read_values16(const uint32_t (&at)[4], u4 (&v)[4]) {
+  u2 r[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(SECOND)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = u4{r[2 * i][0], r[2 * i][1], r[2 * i + 1][0], r[2 * i + 1][1]};
+}
+__device__ __forceinline__ void read_values8(const uint32_t (&at)[4], u4 (&v)[4]) {
+  u2 r[4];
+  asm volatile(
+      "ds_read_b64_tr_b8 %0, %4\n\tds_read_b64_tr_b8 %1, %5\n\tds_read_b64_tr_b8 %2, %6\n\tds_read_b64_tr_b8 %3, %7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = u4{r[i][0], r[i][1], 0, 0};
+}
+__device__ __forceinline__ uint32_t lds_address(const char *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
 }
 template <bool BF16>
 __device__ __forceinline__ uint16_t narrow(float f) {
   return BF16 ? __builtin_bit_cast(uint16_t, (__bf16)f) : __builtin_bit_cast(uint16_t, (_Float16)f);
 }
 
+template <bool BF16>
+__device__ __forceinline__ float wide(uint16_t h) {
+  return BF16 ? __uint_as_float((uint32_t)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+}
+
+// BF16: the type of the queries and the output, and of a 16-bit cache.
 template <int D, bool BF16, bool I8>
 __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const PagedParams p) {
   using C = PagedCfg<D, I8>;
   constexpr int KS = D / 32, DT = D / 16;
+  constexpr bool MB = BF16 && !I8;  // the matrix instructions' type
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const int split = blockIdx.x, h = blockIdx.y / p.tiles, ht = blockIdx.y % p.tiles, b = blockIdx.z;
+  // key heads vary fastest: their workgroups read neighbouring pieces of the same pages at about the same time (16 requests, 8 key
+  // heads of 256, pages of 64: 137 us with the splits fastest, 107 so)
+  const int split = blockIdx.y, h = blockIdx.x / p.tiles, ht = blockIdx.x % p.tiles, b = blockIdx.z;
+  // The pages' numbers need the request's length only for what lies beyond it, so without a window both loads go out together.
+  // Lane 2 i + a: block a (16 tokens) of the wavefront's tile 32 n + i
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  auto page_of = [&](int first_tile, int j) {
+    const int64_t col = (int64_t)(2 * (first_tile + wave + kPagedWaves * (j + (lane >> 1))) + (lane & 1)) >> (p.shift - 4);
+    return col < p.cols ? p.table[b * p.ldt + col] : -1;
+  };
+  int raw = p.window == 0 ? page_of(split * p.split_tiles, 0) : -1;
   const Span span(p, b);
   const int heads = p.group - ht * kPagedHeads < kPagedHeads ? p.group - ht * kPagedHeads : kPagedHeads;
   const int head0 = h * p.group + ht * kPagedHeads;
-  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   uint16_t *out = reinterpret_cast<uint16_t *>(p.out) + b * p.ldo + (int64_t)head0 * D;
   if (split >= span.used) {
     if (split == 0)  // nothing is seen
@@ -170,59 +218,85 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
   const int mine = (nt - wave + kPagedWaves - 1) / kPagedWaves;  // at least 0
   char *kbuf = smem + wave * C::WAVE, *vbuf = kbuf + C::TILE, *sbuf = vbuf + C::TILE;
 
+  // -1: not a page, or not a token
+  int ids = -1;
+  auto take_ids = [&](int j) {
+    const int blk = 2 * (t0 + wave + kPagedWaves * (j + (lane >> 1))) + (lane & 1);
+    ids = (int64_t)blk * 16 < span.len && raw >= 0 && raw < p.n_pages ? raw : -1;
+  };
+  if (p.window != 0) raw = page_of(t0, 0);
+  take_ids(0);
+
+  // ---- queries.  Lane group `quad` holds the dims of its chunk of each step (any order serves, if keys and queries share it)
   u4 fq[KS];
+  float c = p.c;  // of this lane's head
   {
     const char *qrow = p.q + (b * p.ldq + (int64_t)(head0 + (l16 < heads ? l16 : 0)) * D) * 2;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const int dim = I8 ? 16 * (4 * (s >> 1) + quad) + 8 * (s & 1) : 8 * (4 * s + quad);
       fq[s] = *reinterpret_cast<const u4 *>(qrow + dim * 2);
+      if (p.negate) fq[s] ^= 0x80008000u;
       if (l16 >= heads) fq[s] = u4{0, 0, 0, 0};
+    }
+    if (I8 && BF16) {  // to binary16, relative to 2^e > max |q|
+      float top = 0x1p-126f;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          top = fmaxf(top, fmaxf(fabsf(__uint_as_float(fq[s][i] << 16)), fabsf(__uint_as_float(fq[s][i] & 0xffff0000u))));
+      const int e = __builtin_amdgcn_frexp_expf(quad_max(top));
+      c = fmaxf(__builtin_amdgcn_ldexpf(c, e), 0x1p-126f);
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = __builtin_amdgcn_ldexpf(__uint_as_float(fq[s][i] << 16), -e);
+          const float y = __builtin_amdgcn_ldexpf(__uint_as_float(fq[s][i] & 0xffff0000u), -e);
+          fq[s][i] = (uint32_t)narrow<false>(x) | (uint32_t)narrow<false>(y) << 16;
+        }
     }
   }
 
-  // ---- pages: lane 2 i + a holds that of block a (16 tokens) of the wavefront's tile 32 n + i; -1: not a page, or not a token
-  int ids = -1;
-  auto fetch_ids = [&](int j) {
-    const int blk = 2 * (t0 + wave + kPagedWaves * (j + (lane >> 1))) + (lane & 1);
-    const int64_t col = (int64_t)blk >> (p.shift - 4);
-    ids = -1;
-    if (col < p.cols && (int64_t)blk * 16 < span.len) {
-      const int id = p.table[b * p.ldt + col];
-      if (id >= 0 && id < p.n_pages) ids = id;
-    }
-  };
-  // row of the cache [page, head, token] at which the 16 tokens start; a missing page's loads go to page 0
+  // row of the cache [page, head, token] at which 16 tokens start; a missing page's loads go to page 0
   auto row_of = [&](int id, int blk) {
     return (((int64_t)(id < 0 ? 0 : id) * p.kv_heads + h) << p.shift) + ((blk * 16) & ((1 << p.shift) - 1));
   };
-  const int lr = lane / C::CPR;
-  const uint32_t voff = (uint32_t)(lr * C::RB + (((lane % C::CPR) ^ C::swz(lr)) << 4));
-  auto issue = [&](const char *cache, const float *scales, int idA, int idB, int tile, char *dst, char *sdst) {
-    const int64_t ra = row_of(idA, 2 * tile), rb = row_of(idB, 2 * tile + 1);
+  uint32_t voff[C::LB];
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      const char *src = cache + (a ? rb : ra) * C::RB;
+  for (int i = 0; i < C::LB; ++i) {
+    const int r = i * (1024 / C::RB) + lane / C::CPR;
+    voff[i] = (uint32_t)(r * C::RB + (((lane % C::CPR) ^ C::swz(r)) << 4));
+  }
+  auto issue = [&](const char *cache, const float *scales, int64_t ra, int64_t rb, char *dst, char *sdst) {
+    const char *src[2] = {cache + ra * C::RB, cache + rb * C::RB};
 #pragma unroll
-      for (int i = 0; i < C::LB; ++i)  // rows (1024 / RB) i + lr: their swizzle is the XOR of the parts'
-        to_lds16(src + i * 1024 + (voff ^ (uint32_t)(C::swz(i * (1024 / C::RB)) << 4)), dst + a * C::BLOCK + i * 1024);
-    }
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int i = 0; i < C::LB; ++i) to_lds16(src[a], voff[i], dst + a * C::BLOCK + i * 1024);
     if (I8) to_lds4(scales + (lane & 16 ? rb : ra) + l16, sdst);
   };
+  // a lane's place in the transposing reads.  16 bit: four rows (tokens 4 quad .. + 3 of a block) x 16 dims, lane = row l16 / 4,
+  // quarter l16 % 4; 8 bit: eight rows (tokens 4 quad .. + 3 of both blocks) x 16 dims, lane = row l16 / 2, half l16 % 2.
+  // Its chunk of dims 16 t .. is 2 t + (l16 % 4) / 2, or t: the part that depends on t is XORed with the rest
+  const int v_token = I8 ? ((l16 >> 1) < 4 ? 0 : 16) + 4 * quad + ((l16 >> 1) & 3) : 4 * quad + (l16 >> 2);
+  const uint32_t v_at = lds_address(vbuf) + v_token * C::RB + (l16 & 1) * 8;
+  const uint32_t v_swz = (uint32_t)((I8 ? 0 : (l16 & 3) >> 1) ^ C::swz(v_token & 15)) << 4;
 
   v4f acc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) acc[i] = v4f{0, 0, 0, 0};
-  float m = -INFINITY, l = 0.0f;
-  int ref = -1000;  // exponent of the unit of acc (8-bit caches)
+  float m = -INFINITY, l = 0.0f;  // maximum of the logits before the factor c, sum of the weights of this lane's tokens
+  float unit = 0x1p-126f, per_unit = 0x1p126f;  // of acc (8-bit caches): a power of two above every value scale so far
 
   int idA = -1, idB = -1;
   if (mine > 0) {
-    fetch_ids(0);
     idA = __builtin_amdgcn_readlane(ids, 0);
     idB = __builtin_amdgcn_readlane(ids, 1);
-    issue(p.k, p.ks, idA, idB, t0 + wave, kbuf, sbuf);
-    issue(p.v, p.vs, idA, idB, t0 + wave, vbuf, sbuf + C::SCALES);
+    const int64_t ra = row_of(idA, 2 * (t0 + wave)), rb = row_of(idB, 2 * (t0 + wave) + 1);
+    issue(p.k, p.ks, ra, rb, kbuf, sbuf);
+    issue(p.v, p.vs, ra, rb, vbuf, sbuf + C::SCALES);
   }
 #pragma unroll 1
   for (int j = 0; j < mine; ++j) {
@@ -246,12 +320,19 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
       }
     }
     wait_lds();
+    int64_t ra = 0, rb = 0;
     int nextA = -1, nextB = -1;
     if (more) {
-      if (((j + 1) & 31) == 0) fetch_ids(j + 1);
-      nextA = __builtin_amdgcn_readlane(ids, 2 * ((j + 1) & 31));
-      nextB = __builtin_amdgcn_readlane(ids, 2 * ((j + 1) & 31) + 1);
-      issue(p.k, p.ks, nextA, nextB, tile + kPagedWaves, kbuf, sbuf);
+      const int n = (j + 1) & 31;
+      if (n == 0) {
+        raw = page_of(t0, j + 1);
+        take_ids(j + 1);
+      }
+      nextA = __builtin_amdgcn_readlane(ids, 2 * n);
+      nextB = __builtin_amdgcn_readlane(ids, 2 * n + 1);
+      ra = row_of(nextA, 2 * (tile + kPagedWaves));
+      rb = row_of(nextB, 2 * (tile + kPagedWaves) + 1);
+      issue(p.k, p.ks, ra, rb, kbuf, sbuf);
     }
     v4f s[2] = {v4f{0, 0, 0, 0}, v4f{0, 0, 0, 0}};
 #pragma unroll
@@ -259,21 +340,20 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
       if (I8) {
 #pragma unroll
         for (int u = 0; u < KS / 2; ++u) {
-          s[a] = mma<BF16>(widen<BF16>(fk[a][u][0], fk[a][u][1]), fq[2 * u], s[a]);
-          s[a] = mma<BF16>(widen<BF16>(fk[a][u][2], fk[a][u][3]), fq[2 * u + 1], s[a]);
+          s[a] = mma<MB>(widen(fk[a][u][0], fk[a][u][1]), fq[2 * u], s[a]);
+          s[a] = mma<MB>(widen(fk[a][u][2], fk[a][u][3]), fq[2 * u + 1], s[a]);
         }
       } else {
 #pragma unroll
-        for (int t = 0; t < KS; ++t) s[a] = mma<BF16>(fk[a][t], fq[t], s[a]);
+        for (int t = 0; t < KS; ++t) s[a] = mma<MB>(fk[a][t], fq[t], s[a]);
       }
     }
     settle();
-#pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      if (I8) s[a] *= ksc[a];
-      s[a] *= p.c;
-    }
     // ---- weights.  Element i of s[a] is token 32 tile + 16 a + 4 quad + i of head l16.
+    if (I8) {
+#pragma unroll
+      for (int a = 0; a < 2; ++a) s[a] *= ksc[a];
+    }
     const bool whole = okA && okB && tile * kPagedTile >= span.lo && tile * kPagedTile + kPagedTile <= span.len;
     uint32_t seen = 0xff;  // bit 4 a + i
     if (!whole) {
@@ -295,15 +375,16 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
       for (int i = 0; i < 4; ++i) top = fmaxf(top, s[a][i]);
     const float m_new = fmaxf(m, quad_max(top));
     const float base = m_new == -INFINITY ? 0.0f : m_new;
-    float alpha = __builtin_amdgcn_exp2f(m - base);
+    float alpha = __builtin_amdgcn_exp2f((m - base) * c);
     m = m_new;
     l *= alpha;
+    const float shift = -base * c;
     float w[8];
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        w[4 * a + i] = __builtin_amdgcn_exp2f(s[a][i] - base);
+        w[4 * a + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[a][i], c, shift));
         l += w[4 * a + i];
       }
 
@@ -315,29 +396,24 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
     u4 fv[DT];
     v4f vsc[2];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) {
-      if (I8) {
-        // eight rows (tokens 4 quad .. + 3 of both blocks) x 16 dims: lane = row l16 / 2, half l16 % 2
-        const int r = l16 >> 1, token = (r < 4 ? 0 : 16) + 4 * quad + (r & 3);
-        const char *at = vbuf + token * C::RB + ((t ^ C::swz(token & 15)) << 4) + (l16 & 1) * 8;
-        const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i *)(at));
-        fv[t][0] = (uint32_t)x[0], fv[t][1] = (uint32_t)x[1];
-      } else {
-        // per block four rows (tokens 4 quad .. + 3) x 16 dims: lane = row l16 / 4, quarter l16 % 4
-        const int r = 4 * quad + (l16 >> 2);
-        const char *at = vbuf + r * C::RB + (((2 * t + ((l16 & 3) >> 1)) ^ C::swz(r)) << 4) + (l16 & 1) * 8;
-        const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(at));
-        const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(at + C::BLOCK));
-        const u2 xu = __builtin_bit_cast(u2, x), yu = __builtin_bit_cast(u2, y);
-        fv[t] = u4{xu[0], xu[1], yu[0], yu[1]};
-      }
+    for (int t0 = 0; t0 < DT; t0 += 4) {
+      uint32_t at[4];
+      u4 four[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) at[i] = v_at + (((uint32_t)(t0 + i) * (I8 ? 16 : 32)) ^ v_swz);
+      if constexpr (I8)
+        read_values8(at, four);
+      else
+        read_values16<C::BLOCK>(at, four);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) fv[t0 + i] = four[i];
     }
     if (I8) {
 #pragma unroll
       for (int a = 0; a < 2; ++a) vsc[a] = *reinterpret_cast<const v4f *>(sbuf + C::SCALES + (a * 16 + 4 * quad) * 4);
     }
     wait_lds();
-    if (more) issue(p.v, p.vs, nextA, nextB, tile + kPagedWaves, vbuf, sbuf + C::SCALES);
+    if (more) issue(p.v, p.vs, ra, rb, vbuf, sbuf + C::SCALES);
     if (!whole) {  // what lies at tokens that are not seen may be anything
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
@@ -351,39 +427,42 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
           for (int i = 0; i < 8; ++i) fv[t][i >> 1] &= (seen >> i) & 1 ? ~0u : ~(0xffffu << (16 * (i & 1)));
         }
       }
+      if (I8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (!((seen >> i) & 1)) vsc[i >> 2][i & 3] = 0.0f;
+      }
     }
     if (I8) {
-      float big = 0x1p-126f;
+      float big = 0.0f;
 #pragma unroll
-      for (int a = 0; a < 2; ++a)
+      for (int i = 0; i < 8; ++i) big = fmaxf(big, vsc[i >> 2][i & 3]);
+      if (__builtin_amdgcn_ballot_w64(big > unit)) {  // rare: a larger scale than any before
+        const int e = __builtin_amdgcn_frexp_expf(fmaxf(quad_max(big), unit));
+        const float next = e < 126 ? __builtin_amdgcn_ldexpf(1.0f, e) : 0x1p126f;
+        alpha *= unit / next;
+        unit = next;
+        per_unit = 1.0f / next;
+      }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (!whole && !((seen >> (4 * a + i)) & 1)) vsc[a][i] = 0.0f;
-          big = fmaxf(big, vsc[a][i]);
-        }
-      const int e = __builtin_amdgcn_frexp_expf(quad_max(big));
-      const int unit = e > ref ? e : ref;
-      alpha = __builtin_amdgcn_ldexpf(alpha, ref - unit);
-      ref = unit;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] *= __builtin_amdgcn_ldexpf(vsc[i >> 2][i & 3], -unit);
+      for (int i = 0; i < 8; ++i) w[i] *= vsc[i >> 2][i & 3] * per_unit;
     }
     u4 hi, lo;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint16_t a0 = narrow<BF16>(w[2 * i]), a1 = narrow<BF16>(w[2 * i + 1]);
+      const uint16_t a0 = narrow<MB>(w[2 * i]), a1 = narrow<MB>(w[2 * i + 1]);
       hi[i] = (uint32_t)a0 | (uint32_t)a1 << 16;
-      if (BF16) {
-        const float r0 = w[2 * i] - __uint_as_float((uint32_t)a0 << 16), r1 = w[2 * i + 1] - __uint_as_float((uint32_t)a1 << 16);
-        lo[i] = (uint32_t)narrow<BF16>(r0) | (uint32_t)narrow<BF16>(r1) << 16;
-      }
+      if (!I8) lo[i] = (uint32_t)narrow<MB>(w[2 * i] - wide<MB>(a0)) | (uint32_t)narrow<MB>(w[2 * i + 1] - wide<MB>(a1)) << 16;
+    }
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {  // after the first tiles a maximum seldom moves
+#pragma unroll
+      for (int t = 0; t < DT; ++t) acc[t] *= alpha;
     }
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
-      const u4 val = I8 ? widen<BF16>(fv[t][0], fv[t][1]) : fv[t];
-      acc[t] *= alpha;
-      acc[t] = mma<BF16>(val, hi, acc[t]);
-      if (BF16) acc[t] = mma<BF16>(val, lo, acc[t]);
+      const u4 val = I8 ? widen(fv[t][0], fv[t][1]) : fv[t];
+      acc[t] = mma<MB>(val, hi, acc[t]);
+      if (!I8) acc[t] = mma<MB>(val, lo, acc[t]);
     }
     settle();
     idA = nextA;
@@ -399,14 +478,11 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
 #pragma unroll
   for (int t = 0; t < DT; ++t) {
     v4f o = acc[t];
-    if (I8) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_ldexpf(o[i], ref);
-    }
+    if (I8) o *= unit;
     *reinterpret_cast<v4f *>(mine_at + 16 * t) = o;
   }
   if (quad == 0) {
-    ml[(wave * kPagedHeads + l16) * 2] = m;
+    ml[(wave * kPagedHeads + l16) * 2] = m * c;
     ml[(wave * kPagedHeads + l16) * 2 + 1] = l;
   }
   __syncthreads();
@@ -441,35 +517,51 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
   }
 }
 
-// The parts of a split length: one workgroup per request and query head.
+// The parts of a split length: one workgroup per request and query head.  Bound: latency; so D / 4 threads read a part in 16-byte
+// pieces, the workgroup's 256 D / 4 groups of them take turns over the parts with several loads in flight, and every
+// wavefront works out the parts' factors for itself.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedParams p) {
-  constexpr int G = 256 / D;  // groups of D threads, which take turns over the splits
-  __shared__ float f_s[kPagedMaxSplits], l_s[kPagedMaxSplits], o_s[G][D];
-  const int head = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  constexpr int G = 1024 / D;
+  constexpr int PER = kPagedMaxSplits / 64;  // parts per lane
+  __shared__ float factor[kPagedMaxSplits];
+  __shared__ v4f part[G][D / 4];
+  const int head = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
   const Span span(p, b);
-  if (span.used <= 1) return;
+  const int n = span.used;
+  if (n <= 1) return;
   const int64_t at = ((int64_t)b * p.q_heads + head) * p.splits;
-  const float *pml = p.part + (int64_t)p.batch * p.q_heads * p.splits * D + at * 2;
-  for (int s = tid; s < span.used; s += 256) {
-    f_s[s] = pml[2 * s];
-    l_s[s] = pml[2 * s + 1];
-  }
-  __syncthreads();
-  float top = -INFINITY;
-  for (int s = 0; s < span.used; ++s) top = fmaxf(top, f_s[s]);
-  const float base = top == -INFINITY ? 0.0f : top;
-  float o = 0.0f, sum = 0.0f;
-  const int d = tid % D, g = tid / D;
-  for (int s = g; s < span.used; s += G) o += __builtin_amdgcn_exp2f(f_s[s] - base) * p.part[(at + s) * D + d];
-  o_s[g][d] = o;
-  for (int s = 0; s < span.used; ++s) sum += __builtin_amdgcn_exp2f(f_s[s] - base) * l_s[s];
-  __syncthreads();
-  if (g == 0) {
+  const float2 *pml = reinterpret_cast<const float2 *>(p.part + (int64_t)p.batch * p.q_heads * p.splits * D) + at;
+  float2 x[PER];
+  float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int i = 1; i < G; ++i) o += o_s[i][d];
-    if (sum == 0.0f) sum = 1.0f;
-    reinterpret_cast<uint16_t *>(p.out)[b * p.ldo + (int64_t)head * D + d] = narrow<BF16>(o / sum);
+  for (int i = 0; i < PER; ++i) {
+    x[i] = lane + 64 * i < n ? pml[lane + 64 * i] : make_float2(-INFINITY, 0.0f);
+    top = fmaxf(top, x[i].x);
+  }
+  top = wave_max(top);
+  const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const float f = __builtin_amdgcn_exp2f(x[i].x - base);
+    sum += f * x[i].y;
+    if (tid < 64) factor[lane + 64 * i] = f;
+  }
+  sum = wave_sum(sum);
+  if (sum == 0.0f) sum = 1.0f;  // no token with a page: zeros
+  __syncthreads();
+  const int d4 = tid % (D / 4), g = tid / (D / 4);
+  const v4f *src = reinterpret_cast<const v4f *>(p.part + at * D) + d4;
+  v4f o = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int s = g; s < n; s += G) o += factor[s] * src[(int64_t)s * (D / 4)];
+  part[g][d4] = o;
+  __syncthreads();
+  if (tid < D) {
+    float r = 0.0f;
+#pragma unroll
+    for (int i = 0; i < G; ++i) r += reinterpret_cast<const float *>(part[i])[tid];
+    reinterpret_cast<uint16_t *>(p.out)[b * p.ldo + (int64_t)head * D + tid] = narrow<BF16>(r / sum);
   }
 }
 
@@ -480,7 +572,7 @@ cwac_status launch_paged(const PagedParams &p, hipStream_t st) {
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attention_kernel<D, BF16, I8>),
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (attr != hipSuccess) return CWAC_E_LAUNCH;
-  paged_attention_kernel<D, BF16, I8><<<dim3(p.splits, p.kv_heads * p.tiles, p.batch), 64 * kPagedWaves, LDS, st>>>(p);
+  paged_attention_kernel<D, BF16, I8><<<dim3(p.kv_heads * p.tiles, p.splits, p.batch), 64 * kPagedWaves, LDS, st>>>(p);
   const cwac_status s = launch_status();
   if (s != CWAC_OK || p.splits == 1) return s;
   paged_join_kernel<D, BF16><<<dim3(p.q_heads, p.batch), 256, 0, st>>>(p);
@@ -543,7 +635,8 @@ extern "C" cwac_status llm_paged_attention(const void *q, int64_t ldq, int32_t t
   p.q = static_cast<const char *>(q), p.k = static_cast<const char *>(k_cache), p.v = static_cast<const char *>(v_cache);
   p.ks = k_scales, p.vs = v_scales, p.table = table, p.lens = lens, p.out = static_cast<char *>(out);
   p.part = static_cast<float *>(workspace);
-  p.ldq = ldq, p.ldo = ldo, p.ldt = ldt, p.c = scale * 1.44269504088896340736f;
+  p.ldq = ldq, p.ldo = ldo, p.ldt = ldt, p.c = fabsf(scale) * 1.44269504088896340736f, p.negate = scale < 0.0f;
+  if (p.c < 0x1p-126f) p.c = 0x1p-126f;  // a masked logit stays -inf when the scale is zero
   p.batch = batch, p.q_heads = q_heads, p.kv_heads = kv_heads, p.group = q_heads / kv_heads;
   p.tiles = (p.group + kPagedHeads - 1) / kPagedHeads;
   for (p.shift = 4; (1 << p.shift) < page;) ++p.shift;

@@ -11,14 +11,21 @@ constexpr int kPagedWaves = 4;    // wavefronts of a workgroup: they take turns 
 constexpr int kPagedHeads = 16;   // query heads of one key head that share a workgroup: the columns of the matrix instruction
 constexpr int kPagedMaxSplits = 128;
 
-// Splits of `tokens` positions: as many as fill the chip four times with workgroups, none shorter than a turn of its wavefronts.
+// Splits of `tokens` positions.  A workgroup has a fixed cost of 1.6 us (its first loads, the join), so splits are long, 1024
+// tokens, where there are enough of them - at most 4096 workgroups, for requests of uneven lengths - and shorter only to fill the chip
+// with workgroups (two per compute unit, twice), down to a turn of the wavefronts.  Measured in us with at most 1024 / 2048 / 4096 workgroups and
+// splits of 128 tokens or more: 61 requests of 1 to 8190 tokens, 8 key heads, bf16 192 / 189 / 189; 5 of 30011 to 131072, int8
+// 187 / 170 / 164; 256 of 100 to 1900 190 / 190 / 207 (split in two); 8 of 2000, 32 key heads 51 / 52 / 60; 16 of 100 to 8000,
+// heads of 256 101 / 107 / 116; 64 of 100 to 6000, int8 heads of 64 61 / 60 / 53; one of 131072, one key head 17.8 at 128 splits, 19.7 at 256.
 inline int paged_splits(int64_t batch, int q_heads, int kv_heads, int64_t tokens) {
   const int group = q_heads / kv_heads, tiles = (group + kPagedHeads - 1) / kPagedHeads;
   const int64_t rows = batch * kv_heads * tiles, turn = kPagedTile * kPagedWaves;
-  int64_t most = (tokens + turn - 1) / turn, want = (2048 + rows - 1) / rows;
-  if (want > kPagedMaxSplits) want = kPagedMaxSplits;
-  if (want < most) most = want;
-  return most < 1 ? 1 : (int)most;
+  int64_t fill = (1024 + rows - 1) / rows, turns = (tokens + turn - 1) / turn;
+  if (turns < fill) fill = turns;
+  int64_t even = 4096 / rows;
+  if (tokens / 1024 < even) even = tokens / 1024;
+  const int64_t most = fill > even ? fill : even;
+  return most < 1 ? 1 : (most > kPagedMaxSplits ? kPagedMaxSplits : (int)most);
 }
 // Tokens of one split: whole turns.
 inline int64_t paged_chunk(int64_t tokens, int splits) {

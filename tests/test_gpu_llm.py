@@ -171,16 +171,21 @@ def _run(q, k, v, ks, vs, table, lens, scale, window, page):
 def _check(out, q, k, v, ks, vs, table, lens, scale, window, t):
     """Bound of the error: the output's rounding; a weight's (binary16: half a step, and half its smallest step next to the largest
     weight 1; two bfloat16 terms: 2^-16); the logits' fp32 sums, products and exponential, which enter a weight
-    relatively and both sums; fp32 sums over the tokens.  All of them times sum w |v|, the smallest step times max |v|."""
+    relatively and both sums; fp32 sums over the tokens.  All of them times sum w |v|, the smallest step times max |v|.
+    8-bit caches: weights are binary16 for either type, and bfloat16 queries become binary16 relative to 2^e <= 2 max |q|, each off by
+    at most half its smallest step, 2^-25 * 2^e."""
     kn, vn = _numbers(k, ks), _numbers(v, vs)
     d = q.shape[2]
     want, mag, seen, qk = orc.attention(q.double().cpu().numpy(), kn, vn, table.cpu().numpy(), lens.cpu().numpy(), scale, window,
                                         q.shape[1] // k.shape[1])
-    weight = 2.0 ** -11 if t == "f16" else 2.0 ** -16
+    weight = 2.0 ** -11 if t == "f16" or k.dtype == torch.int8 else 2.0 ** -16
     logit = (d / 16 + 8) * 2.0 ** -23 * (qk + 1.0)
+    half = t == "f16" or k.dtype == torch.int8
+    if t == "bf16" and half:
+        logit = logit + d * 2.0 ** -24 * float(q.abs().max()) * np.nan_to_num(np.abs(kn)).max() * abs(scale)
     rel = weight + 2 * logit + 2.0 ** -23 * (seen[:, None] + 16)
     vmax = np.nan_to_num(np.abs(vn)).max()
-    tol = EPS[t] * np.abs(want) + rel[..., None] * mag * 1.01 + (seen[:, None, None] * 2.0 ** -24 * vmax if t == "f16" else 0.0) + \
+    tol = EPS[t] * np.abs(want) + rel[..., None] * mag * 1.01 + (seen[:, None, None] * 2.0 ** -24 * vmax if half else 0.0) + \
         (2.0 ** -25 if t == "f16" else 0.0)
     got = out.double().cpu().numpy()
     assert np.isfinite(got).all()
