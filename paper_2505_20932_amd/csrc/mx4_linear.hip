@@ -290,15 +290,18 @@ cwac_status launch_split(Mx4Params p, int out_kind, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Many tiles: BM tokens x BN channels per workgroup, both panels through a ring of NSTAGE stages in LDS, one stage = one panel of 256
+// Many tiles: BM tokens x BN channels at a time, both panels through a ring of NSTAGE stages in LDS, one stage = one panel of 256
 // values (128 bytes of codes and 8 scale bytes per row).  Bound: the matrix cores, under the device's power limit.
 //   * Codes go global -> LDS directly, 8 rows x 128 bytes per load; the 16-byte chunk c of row r lands at position c ^ ((r >> 1) & 7)
-//     (applied on the global side), so operand reads are free of bank conflicts.  Buffer loads: what lies
-//     beyond the matrix reads as zeros, so the last panel needs no case of its own.
+//     (applied on the global side), so operand reads are free of bank conflicts.  Buffer loads whose descriptor moves along K with
+//     the stages and ends with the matrix: a lane's offset never changes, and what lies beyond reads as zeros, so the last
+//     panel needs no case of its own.
 //   * A stage is four steps of v_mfma_scale_f32_32x32x64: the half-wave h takes block 4 h + step of its row, so its four scale bytes
 //     are one word, read once per stage, and the instruction picks the step's byte.
 //   * Operands are double-buffered in registers: the LDS reads of a step run under the matrix instructions of the one before,
 //     those of the next stage's first step under this stage's last, behind the only barrier of the stage.
+//   * Workgroups are persistent: the first stage of the next tile and its parameters travel under the epilogue, whose slabs lie over the
+//     other stages.
 // Tiles that reach beyond the matrix are moved inwards: their rows or channels are computed twice, with the same values.
 // ------------------------------------------------------------------------------------------
 template <int BM_, int BN_, int WM_, int TA_, int NSTAGE_>
@@ -307,16 +310,20 @@ struct Mx4TileCfg {
   static constexpr int WM = WM_, WN = BN / (32 * TA), NW = WM * WN, NT = 64 * NW;
   static constexpr int TB = BM / (32 * WM);                             // 32-token tiles per wavefront
   static constexpr int BK = kMx4Panel / 2;
-  static constexpr int X_BYTES = BM * BK, W_BYTES = BN * BK, CODES = X_BYTES + W_BYTES;
-  static constexpr int STAGE = CODES + (BM + BN) * 8;                   // codes, scale bytes of the tokens, of the channels
+  // LDS: codes of the tokens [NSTAGE], of the channels [NSTAGE], their scale bytes [NSTAGE] each, two parameter blocks
+  static constexpr int X_BYTES = BM * BK, W_BYTES = BN * BK, W_AT = NSTAGE * X_BYTES, XS_AT = W_AT + NSTAGE * W_BYTES;
+  static constexpr int WS_AT = XS_AT + NSTAGE * BM * 8, PARAM = WS_AT + NSTAGE * BN * 8, LDS = PARAM + 2 * 8 * BN;
   static constexpr int XR = BM / NW, WR = BN / NW;                      // rows whose loads a wavefront issues
   static constexpr int LX = XR / 8, LW = WR / 8, SX = XR / 32, SW = WR / 32, LPS = LX + LW + SX + SW;
-  static constexpr int PARAM = NSTAGE * STAGE;                          // multiplier, constant [BN]
-  static constexpr int SLAB = 32 * 272;                                 // of the epilogue: 32 rows x 256 bytes, 16 apart
-  static constexpr int LDS = PARAM + 8 * BN;
-  static_assert(XR % 32 == 0 && WR % 32 == 0 && (NSTAGE - 1) * LPS < 64 && NW * SLAB <= PARAM && LDS <= 160 * 1024, "layout");
+  // slabs of the epilogue, 8 KiB each, over stage 1 of the tokens (the first half of the wavefronts) and of the channels
+  static constexpr int SLAB = 8192;
+  static_assert(XR % 32 == 0 && WR % 32 == 0 && LDS <= 160 * 1024 && NSTAGE * BM * BK <= 65536 && NSTAGE * BN * BK <= 65536, "layout");
+  static_assert(NW / 2 * SLAB <= X_BYTES && NW / 2 * SLAB <= W_BYTES && NW == BN / 32 && BN * 4 == NW / 2 * 256, "slabs, parameter loads");
 };
 
+__device__ __forceinline__ void words_to_lds(__amdgpu_buffer_rsrc_t desc, uint8_t *dst, int offset) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(desc, CWAC_LDS_PTR(dst), 4, offset, 0, 0, 0);
+}
 template <int STEP>
 __device__ __forceinline__ v16f mfma32(v4i w, v4i x, v16f acc, int ws, int xs) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(w), operand(x), acc, kE2M1, kE2M1, STEP, ws, STEP, xs);
@@ -327,224 +334,265 @@ __global__ __launch_bounds__(C::NT) void mx4_tile_kernel(const Mx4Params p) {
   using O = OutType<OUT>;
   constexpr int TA = C::TA, TB = C::TB, BK = C::BK, NSTAGE = C::NSTAGE;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-  float *s_mult = reinterpret_cast<float *>(smem + C::PARAM), *s_fb = s_mult + C::BN;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wave_m = wave % C::WM, wave_n = wave / C::WM;
-  int tile_m, tile_n;
-  tile_of_block(blockIdx.x, p.tiles_m, p.tiles_n, tile_m, tile_n);
-  int64_t bm0 = (int64_t)tile_m * C::BM;
-  if (bm0 > p.m - C::BM) bm0 = p.m - C::BM;
-  int bn0 = tile_n * C::BN;
-  if (bn0 > p.n - C::BN) bn0 = p.n - C::BN;
-  const __amdgpu_buffer_rsrc_t xd = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint8_t *>(p.x + bm0 * p.ldx), 0, (int)(uint32_t)((uint64_t)(C::BM - 1) * (uint64_t)p.ldx + (uint64_t)(p.k / 2)), 0x00020000);
-  const __amdgpu_buffer_rsrc_t wd = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint8_t *>(p.w + (int64_t)bn0 * p.ldw), 0, (int)(uint32_t)((uint64_t)(C::BN - 1) * (uint64_t)p.ldw + (uint64_t)(p.k / 2)),
-      0x00020000);
-  // a lane's place in a load: row lr of 8, chunk pc ^ swizzle; loads with odd number sit 8 rows further, which flips bit 2 of
-  // the swizzle (a wavefront's rows start at a multiple of 32)
+  const int total = p.tiles_m * p.tiles_n, stages = (p.k + kMx4Panel - 1) / kMx4Panel;
+  if (p.mult == nullptr || p.fbias == nullptr) {  // absent parameters: both blocks filled once
+    for (int i = tid; i < 2 * C::BN; i += C::NT) {
+      float *block = reinterpret_cast<float *>(smem + C::PARAM) + (i / C::BN) * 2 * C::BN;
+      if (!p.mult) block[i % C::BN] = 1.0f;
+      if (!p.fbias) block[C::BN + i % C::BN] = 0.0f;
+    }
+  }
+  // ---- global -> LDS.  A lane's place in a load: row lr of 8, chunk pc ^ swizzle; loads with odd number sit 8 rows further, which
+  // flips bit 2 of the swizzle (a wavefront's rows start at a multiple of 32)
   const int lr = lane >> 3, pc = lane & 7;
-  const uint32_t c0 = (uint32_t)((pc ^ (lr >> 1)) << 4), c1 = c0 ^ 64u;
-  const uint32_t xrow = (uint32_t)(wave * C::XR + lr) * (uint32_t)p.ldx, wrow = (uint32_t)(wave * C::WR + lr) * (uint32_t)p.ldw;
-  const uint32_t xstep = 8u * (uint32_t)p.ldx, wstep = 8u * (uint32_t)p.ldw;
-  const uint8_t *xs = p.xs + (bm0 + wave * C::XR) * 8 + lane * 4, *ws = p.ws + ((int64_t)bn0 + wave * C::WR) * 8 + lane * 4;
-  const int64_t xs_step = p.m * 8, ws_step = (int64_t)p.n * 8;
-  auto issue_x = [&](int buf, int stage) {
-    uint8_t *dst = smem + buf * C::STAGE;
+  int xv[C::LX], wv[C::LW];
 #pragma unroll
-    for (int i = 0; i < C::LX; ++i)
-      codes_to_lds(xd, dst + (wave * C::XR + 8 * i) * BK, (int)(xrow + (uint32_t)i * xstep + ((i & 1) ? c1 : c0) + (uint32_t)(stage * BK)));
+  for (int i = 0; i < C::LX; ++i)
+    xv[i] = (int)((uint32_t)(wave * C::XR + 8 * i + lr) * (uint32_t)p.ldx + (uint32_t)((pc ^ (lr >> 1) ^ ((i & 1) << 2)) << 4));
 #pragma unroll
-    for (int i = 0; i < C::SX; ++i)
-      scales_to_lds(xs + stage * xs_step + i * 256, dst + C::CODES + (wave * C::XR + 32 * i) * 8);
+  for (int i = 0; i < C::LW; ++i)
+    wv[i] = (int)((uint32_t)(wave * C::WR + 8 * i + lr) * (uint32_t)p.ldw + (uint32_t)((pc ^ (lr >> 1) ^ ((i & 1) << 2)) << 4));
+  const int xsv = wave * C::XR * 8 + lane * 4, wsv = wave * C::WR * 8 + lane * 4;
+  int64_t bm0 = 0;
+  int bn0 = 0;
+  // where the next stage to be loaded begins, what is left of the matrix from there, and how many stages are; past the last
+  // one the extents are zero: such loads touch no memory and bring zeros that nobody reads
+  const uint8_t *xg = nullptr, *wg = nullptr, *xsg = nullptr, *wsg = nullptr;
+  uint32_t xleft = 0, wleft = 0;
+  int xtodo = 0, wtodo = 0;
+  auto issue_x = [&](int buf) {
+    const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(xg), 0, xtodo > 0 ? (int)xleft : 0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t ds = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(xsg), 0, xtodo > 0 ? C::BM * 8 : 0, 0x00020000);
+    uint8_t *dst = smem + buf * C::X_BYTES + wave * C::XR * BK;
+#pragma unroll
+    for (int i = 0; i < C::LX; ++i) codes_to_lds(d, dst + i * 8 * BK, xv[i]);
+#pragma unroll
+    for (int i = 0; i < C::SX; ++i) words_to_lds(ds, smem + C::XS_AT + (buf * C::BM + wave * C::XR + 32 * i) * 8, xsv + i * 256);
+    xg += BK, xleft -= BK, xsg += p.m * 8, --xtodo;
   };
-  auto issue_w = [&](int buf, int stage) {
-    uint8_t *dst = smem + buf * C::STAGE;
+  auto issue_w = [&](int buf) {
+    const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(wg), 0, wtodo > 0 ? (int)wleft : 0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t ds = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(wsg), 0, wtodo > 0 ? C::BN * 8 : 0, 0x00020000);
+    uint8_t *dst = smem + C::W_AT + buf * C::W_BYTES + wave * C::WR * BK;
 #pragma unroll
-    for (int i = 0; i < C::LW; ++i)
-      codes_to_lds(wd, dst + C::X_BYTES + (wave * C::WR + 8 * i) * BK,
-                   (int)(wrow + (uint32_t)i * wstep + ((i & 1) ? c1 : c0) + (uint32_t)(stage * BK)));
+    for (int i = 0; i < C::LW; ++i) codes_to_lds(d, dst + i * 8 * BK, wv[i]);
 #pragma unroll
-    for (int i = 0; i < C::SW; ++i)
-      scales_to_lds(ws + stage * ws_step + i * 256, dst + C::CODES + (C::BM + wave * C::WR + 32 * i) * 8);
+    for (int i = 0; i < C::SW; ++i) words_to_lds(ds, smem + C::WS_AT + (buf * C::BN + wave * C::WR + 32 * i) * 8, wsv + i * 256);
+    wg += BK, wleft -= BK, wsg += (int64_t)p.n * 8, --wtodo;
+  };
+  // a tile's origin, its parameters (the first half of the wavefronts the multipliers, the others the constants), its stage 0
+  auto open = [&](int id, int block) {
+    int tile_m, tile_n;
+    tile_of_block(id, p.tiles_m, p.tiles_n, tile_m, tile_n);
+    bm0 = (int64_t)tile_m * C::BM;
+    if (bm0 > p.m - C::BM) bm0 = p.m - C::BM;
+    bn0 = tile_n * C::BN;
+    if (bn0 > p.n - C::BN) bn0 = p.n - C::BN;
+    xg = p.x + bm0 * p.ldx, wg = p.w + (int64_t)bn0 * p.ldw, xsg = p.xs + bm0 * 8, wsg = p.ws + (int64_t)bn0 * 8;
+    xleft = (uint32_t)((uint64_t)(C::BM - 1) * (uint64_t)p.ldx + (uint64_t)(p.k / 2));
+    wleft = (uint32_t)((uint64_t)(C::BN - 1) * (uint64_t)p.ldw + (uint64_t)(p.k / 2));
+    xtodo = wtodo = stages;
+    const float *src = wave < C::NW / 2 ? p.mult : p.fbias;
+    if (src)
+      scales_to_lds(reinterpret_cast<const uint8_t *>(src + bn0 + (wave % (C::NW / 2)) * 64 + lane),
+                    smem + C::PARAM + block * 8 * C::BN + wave * 256);
+    issue_x(0);
+    issue_w(0);
   };
   // ---- LDS -> operands
   const int swz = (l32 >> 1) & 7;
-  const int x_off = (wave_m * 32 * TB + l32) * BK, w_off = C::X_BYTES + (wave_n * 32 * TA + l32) * BK;
-  const int xs_off = C::CODES + (wave_m * 32 * TB + l32) * 8 + 4 * half, ws_off = C::CODES + (C::BM + wave_n * 32 * TA + l32) * 8 + 4 * half;
+  const int x_row = (wave_m * 32 * TB + l32) * BK, w_row = C::W_AT + (wave_n * 32 * TA + l32) * BK;
+  const int xs_row = C::XS_AT + (wave_m * 32 * TB + l32) * 8 + 4 * half, ws_row = C::WS_AT + (wave_n * 32 * TA + l32) * 8 + 4 * half;
   auto read = [&](int buf, int step, v4i(&fw)[TA], v4i(&fx)[TB]) {
-    const uint8_t *base = smem + buf * C::STAGE + (((4 * half + step) ^ swz) << 4);
+    const int chunk = ((4 * half + step) ^ swz) << 4;
 #pragma unroll
-    for (int a = 0; a < TA; ++a) fw[a] = *reinterpret_cast<const v4i *>(base + w_off + a * 32 * BK);
+    for (int a = 0; a < TA; ++a) fw[a] = *reinterpret_cast<const v4i *>(smem + w_row + chunk + buf * C::W_BYTES + a * 32 * BK);
 #pragma unroll
-    for (int b = 0; b < TB; ++b) fx[b] = *reinterpret_cast<const v4i *>(base + x_off + b * 32 * BK);
+    for (int b = 0; b < TB; ++b) fx[b] = *reinterpret_cast<const v4i *>(smem + x_row + chunk + buf * C::X_BYTES + b * 32 * BK);
   };
   auto read_scales = [&](int buf, int(&sw)[TA], int(&sx)[TB]) {
-    const uint8_t *base = smem + buf * C::STAGE;
 #pragma unroll
-    for (int a = 0; a < TA; ++a) sw[a] = *reinterpret_cast<const int *>(base + ws_off + a * 256);
+    for (int a = 0; a < TA; ++a) sw[a] = *reinterpret_cast<const int *>(smem + ws_row + buf * C::BN * 8 + a * 256);
 #pragma unroll
-    for (int b = 0; b < TB; ++b) sx[b] = *reinterpret_cast<const int *>(base + xs_off + b * 256);
+    for (int b = 0; b < TB; ++b) sx[b] = *reinterpret_cast<const int *>(smem + xs_row + buf * C::BM * 8 + b * 256);
   };
   v16f acc[TA][TB];
-#pragma unroll
-  for (int a = 0; a < TA; ++a)
-#pragma unroll
-    for (int b = 0; b < TB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
-  auto mma = [&](auto step, const v4i(&fw)[TA], const v4i(&fx)[TB], const int(&sw)[TA], const int(&sx)[TB]) {
+  v4i fwA[TA], fxA[TB], fwB[TA], fxB[TB];
+  int sw[TA], sx[TB];
+  auto mma = [&](auto step, const v4i(&fw)[TA], const v4i(&fx)[TB]) {
 #pragma unroll
     for (int a = 0; a < TA; ++a)
 #pragma unroll
-      for (int b = 0; b < TB; ++b) acc[a][b] = mfma32<decltype(step)::value>(fw[a], fx[b], acc[a][b], sw[a], sx[b]);
+      for (int b = 0; b < TB; ++b)
+        acc[a][b] = mfma32<decltype(step)::value>(fw[a], fx[b], acc[a][b], sw[a], sx[b]);
   };
-  // one step for the scheduler: the LDS reads behind the first matrix instructions one by one, the loads behind the others
+  // one step for the scheduler: the LDS reads behind the first matrix instructions one or two at a time, the loads behind the others
   auto interleave = [&](int reads, int loads) {
     constexpr int MM = TA * TB;
+    const int each = (reads + MM - 1) / MM;
     int r = reads, l = loads;
 #pragma unroll
     for (int i = 0; i < MM; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      const int rn = (reads + MM - 1) / MM < 1 ? 1 : (reads + MM - 1) / MM;
       if (r > 0) {
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         --r;
-        if (rn > 1 && r > 0) {
+        if (each > 1 && r > 0) {
           __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
           --r;
         }
-      } else if (l > 0) {
-        __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);
-        l -= 2;
+        if (each > 2 && r > 0) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          --r;
+        }
+      }
+      if (l > 0 && i >= MM / 4) {
+        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        --l;
       }
     }
     __builtin_amdgcn_sched_barrier(0);
   };
-
-  const int stages = (p.k + kMx4Panel - 1) / kMx4Panel;
-#pragma unroll
-  for (int s = 0; s < NSTAGE; ++s)
-    if (s < stages) {
-      issue_x(s, s);
-      issue_w(s, s);
-    }
-  for (int i = tid; i < C::BN; i += C::NT) {
-    s_mult[i] = p.mult ? p.mult[bn0 + i] : 1.0f;
-    s_fb[i] = p.fbias ? p.fbias[bn0 + i] : 0.0f;
-  }
-  if (stages >= NSTAGE)
-    wait_loads<(NSTAGE - 1) * C::LPS>();  // (the parameter loads are younger, and waited for by their stores)
-  else
-    wait_loads<0>();
-  __builtin_amdgcn_s_barrier();
-  v4i fwA[TA], fxA[TB], fwB[TA], fxB[TB];
-  int sw[TA], sx[TB];
-  read(0, 0, fwA, fxA);
-  read_scales(0, sw, sx);
   using S0 = std::integral_constant<int, 0>;
   using S1 = std::integral_constant<int, 1>;
   using S2 = std::integral_constant<int, 2>;
   using S3 = std::integral_constant<int, 3>;
   // Stage s in ring place buf.  The loads of stage s + NSTAGE go into the place that this stage leaves, behind its barrier: the
   // tokens' under the last step, the channels' under the first step of the next stage.
-  auto stage_body = [&](int s, int buf, auto steady) {
-    constexpr bool STEADY = decltype(steady)::value;
-    const bool late = STEADY || (s >= 1 && s - 1 + NSTAGE < stages);
+  auto stage_body = [&](int buf) {
     const int prev = buf == 0 ? NSTAGE - 1 : buf - 1, next = buf == NSTAGE - 1 ? 0 : buf + 1;
-    if (late) issue_w(prev, s - 1 + NSTAGE);
+    issue_w(prev);
     read(buf, 1, fwB, fxB);
-    mma(S0{}, fwA, fxA, sw, sx);
-    interleave(TA + TB, late ? C::LW + C::SW : 0);
+    mma(S0{}, fwA, fxA);
+    interleave(TA + TB, C::LW + C::SW);
     read(buf, 2, fwA, fxA);
-    mma(S1{}, fwB, fxB, sw, sx);
+    mma(S1{}, fwB, fxB);
     interleave(TA + TB, 0);
     read(buf, 3, fwB, fxB);
-    mma(S2{}, fwA, fxA, sw, sx);
+    mma(S2{}, fwA, fxA);
     interleave(TA + TB, 0);
-    // stage s + 1 has landed: with NSTAGE > 2 the stages behind it may still travel
-    if (NSTAGE > 2 && (STEADY || s + NSTAGE - 1 < stages))
-      wait_loads<(NSTAGE - 2) * C::LPS>();
-    else
-      wait_loads<0>();
+    wait_loads<(NSTAGE - 2) * C::LPS>();  // stage s + 1 has landed
     wait_lds();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    const bool first = STEADY || s + NSTAGE < stages;
-    if (first) issue_x(buf, s + NSTAGE);
+    issue_x(buf);
     int nw[TA], nx[TB];
-    if (STEADY || s + 1 < stages) {
-      read(next, 0, fwA, fxA);
-      read_scales(next, nw, nx);
-    }
-    mma(S3{}, fwB, fxB, sw, sx);
-    interleave(2 * (TA + TB), first ? C::LX + C::SX : 0);
-    if (STEADY || s + 1 < stages) {
+    read(next, 0, fwA, fxA);
+    read_scales(next, nw, nx);
+    mma(S3{}, fwB, fxB);
+    interleave(2 * (TA + TB), C::LX + C::SX);
 #pragma unroll
-      for (int a = 0; a < TA; ++a) sw[a] = nw[a];
+    for (int a = 0; a < TA; ++a) sw[a] = nw[a];
 #pragma unroll
-      for (int b = 0; b < TB; ++b) sx[b] = nx[b];
-    }
+    for (int b = 0; b < TB; ++b) sx[b] = nx[b];
   };
-  stage_body(0, 0, std::false_type{});
-  int s = 1;
-  // steady state, unrolled over the ring so that its places are compile-time constants
-  for (; s % NSTAGE != 0 && s + NSTAGE < stages; ++s) stage_body(s, s % NSTAGE, std::true_type{});
-  for (; s + 2 * NSTAGE <= stages; s += NSTAGE) {
-#pragma unroll
-    for (int j = 0; j < NSTAGE; ++j) stage_body(s + j, j, std::true_type{});
-  }
-  for (; s < stages; ++s) stage_body(s, s % NSTAGE, std::false_type{});
-  settle();
-  settle();
-  __syncthreads();  // the slabs lie over the ring, in which a late reader may still be
 
-  // ---- epilogue.  Element 4 g + r of acc[a][b]: channel 32 a + 8 g + 4 half + r, token 32 b + l32 of the wavefront's tile.
-  // A slab is 32 tokens x 256 bytes: the channels of 2 (4-byte outputs) or 4 of the 32-channel tiles.
   constexpr int ES = sizeof(typename O::T), AP = ES == 4 ? (TA < 2 ? TA : 2) : TA, ROW = AP * 32 * ES;
-  uint8_t *slab = smem + wave * C::SLAB;
+  constexpr int LPR = ROW / 16, RPS = 64 / LPR, STORES = TB * (TA / AP) * (32 / RPS);  // lanes per row, rows per store, stores per tile
+  constexpr int AHEAD = (NSTAGE - 1) * (C::LX + C::SX) + (NSTAGE - 2) * (C::LW + C::SW);  // loads behind stage 0 when a tile begins
+  static_assert(32 * ROW <= C::SLAB && STORES + AHEAD < 64, "slab, 6-bit counter");
+  uint8_t *slab = smem + (wave < C::NW / 2 ? C::X_BYTES : C::W_AT + C::W_BYTES) + (wave % (C::NW / 2)) * C::SLAB;
+  int id = blockIdx.x, block = 0;
+  bool stored = false;  // this wavefront's newest operations before the stages to come are STORES stores
+  if (id >= total) return;
+  open(id, 0);
+  __syncthreads();  // (the filled parameters)
+  for (;;) {
+    // ---- the tile's first stages.  Operations are counted in order: stage 0 has landed when at most the later ones - and the
+    // stores of the tile before, which lie between - are outstanding
 #pragma unroll
-  for (int b = 0; b < TB; ++b)
-#pragma unroll
-    for (int a0 = 0; a0 < TA; a0 += AP) {
-#pragma unroll
-      for (int a = a0; a < a0 + AP; ++a)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int ch = wave_n * 32 * TA + a * 32 + 8 * g + 4 * half;
-          const v4f mu = *reinterpret_cast<const v4f *>(s_mult + ch), fb = *reinterpret_cast<const v4f *>(s_fb + ch);
-          typename O::T u[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float f = acc[a][b][4 * g + r] * mu[r];
-            if (p.fbias) f = f + fb[r];
-            u[r] = O::make(f);
-          }
-          uint8_t *at = slab + l32 * 272 + ((a - a0) * 32 + 8 * g + 4 * half) * ES;
-          if constexpr (ES == 4)
-            *reinterpret_cast<v4f *>(at) = v4f{u[0], u[1], u[2], u[3]};
-          else
-            *reinterpret_cast<uint2 *>(at) = make_uint2((uint32_t)u[0] | (uint32_t)u[1] << 16, (uint32_t)u[2] | (uint32_t)u[3] << 16);
-        }
-      // (a wavefront's own slab: its LDS operations are in order)
-      typename O::T *o = static_cast<typename O::T *>(p.out) + (bm0 + wave_m * 32 * TB + 32 * b) * p.ldo + bn0 + wave_n * 32 * TA + 32 * a0;
-      if (p.vec_store && ((bn0 * ES) & 15) == 0) {
-        constexpr int LPR = ROW / 16, RPS = 64 / LPR;  // lanes per row, rows per store
-#pragma unroll
-        for (int i = 0; i < 32 / RPS; ++i) {
-          const int row = i * RPS + lane / LPR;
-          *reinterpret_cast<v4i *>(o + row * p.ldo + (lane % LPR) * (16 / ES)) =
-              *reinterpret_cast<const v4i *>(slab + row * 272 + (lane % LPR) * 16);
-        }
-      } else {
-        constexpr int EPR = ROW / ES, RPS = EPR >= 64 ? 1 : 64 / EPR;  // elements per row; whole wavefronts over consecutive ones
-        for (int row = lane / (64 / RPS); row < 32; row += RPS)
-#pragma unroll
-          for (int c = lane % (64 / RPS); c < EPR; c += 64 / RPS)
-            o[row * p.ldo + c] = *reinterpret_cast<const typename O::T *>(slab + row * 272 + c * ES);
-      }
+    for (int s = 1; s < NSTAGE; ++s) {
+      issue_x(s);
+      if (s + 1 < NSTAGE) issue_w(s);
     }
+    if (stored)
+      wait_loads<AHEAD + STORES>();
+    else
+      wait_loads<AHEAD>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int a = 0; a < TA; ++a)
+#pragma unroll
+      for (int b = 0; b < TB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+    read(0, 0, fwA, fxA);
+    read_scales(0, sw, sx);
+    int buf = 0;
+#pragma unroll 1
+    for (int left = stages; left > 0; --left) {
+      stage_body(buf);
+      buf = buf == NSTAGE - 1 ? 0 : buf + 1;
+    }
+    wait_loads<0>();  // the loads past the last stage: their zeros lie where the next tile or the slabs go
+    wait_lds();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    settle();
+    settle();
+
+    // ---- the ring is free: the next tile's first loads go out, then this one's epilogue.  Element 4 g + r of acc[a][b]: channel 32 a + 8 g + 4 half + r, token 32 b + l32 of the wavefront's tile.
+    // A slab is 32 tokens x ROW bytes, the 16-byte chunk c of row r at position c ^ r.
+    const int64_t em0 = bm0;
+    const int en0 = bn0;
+    const float *s_mult = reinterpret_cast<const float *>(smem + C::PARAM + block * 8 * C::BN), *s_fb = s_mult + C::BN;
+    id += gridDim.x;
+    const bool more = id < total;
+    block ^= 1;
+    if (more) open(id, block);
+    const bool whole_lines = p.vec_store && ((en0 * ES) & 15) == 0;
+#pragma unroll
+    for (int b = 0; b < TB; ++b)
+#pragma unroll
+      for (int a0 = 0; a0 < TA; a0 += AP) {
+#pragma unroll
+        for (int a = a0; a < a0 + AP; ++a)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int ch = wave_n * 32 * TA + a * 32 + 8 * g + 4 * half;
+            const v4f mu = *reinterpret_cast<const v4f *>(s_mult + ch), fb = *reinterpret_cast<const v4f *>(s_fb + ch);
+            typename O::T u[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float f = acc[a][b][4 * g + r] * mu[r];
+              if (p.fbias) f = f + fb[r];
+              u[r] = O::make(f);
+            }
+            const int byte = ((a - a0) * 32 + 8 * g + 4 * half) * ES;
+            uint8_t *at = slab + l32 * ROW + (((byte >> 4) ^ (l32 & (LPR - 1))) << 4) + (byte & 15);
+            if constexpr (ES == 4)
+              *reinterpret_cast<v4f *>(at) = v4f{u[0], u[1], u[2], u[3]};
+            else
+              *reinterpret_cast<uint2 *>(at) = make_uint2((uint32_t)u[0] | (uint32_t)u[1] << 16, (uint32_t)u[2] | (uint32_t)u[3] << 16);
+          }
+        // (a wavefront's own slab: its LDS operations are in order)
+        typename O::T *o = static_cast<typename O::T *>(p.out) + (em0 + wave_m * 32 * TB + 32 * b) * p.ldo + en0 + wave_n * 32 * TA + 32 * a0;
+        if (whole_lines) {
+#pragma unroll
+          for (int i = 0; i < 32 / RPS; ++i) {
+            const int row = i * RPS + lane / LPR;
+            *reinterpret_cast<v4i *>(o + row * p.ldo + (lane % LPR) * (16 / ES)) =
+                *reinterpret_cast<const v4i *>(slab + row * ROW + (((lane % LPR) ^ (row & (LPR - 1))) << 4));
+          }
+        } else {  // whole wavefronts over consecutive elements of a row
+          constexpr int EPR = ROW / ES, LANES = EPR < 64 ? EPR : 64;
+          for (int row = lane / LANES; row < 32; row += 64 / LANES)
+#pragma unroll
+            for (int e = lane % LANES; e < EPR; e += LANES)
+              o[row * p.ldo + e] =
+                  *reinterpret_cast<const typename O::T *>(slab + row * ROW + ((((e * ES) >> 4) ^ (row & (LPR - 1))) << 4) + ((e * ES) & 15));
+        }
+      }
+    if (!more) break;
+    stored = whole_lines;
+    wait_lds();
+    __builtin_amdgcn_s_barrier();  // every slab is read: the stages under them are free
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
 template <typename C, int OUT>
@@ -560,11 +608,14 @@ template <typename C>
 cwac_status launch_tile(Mx4Params p, int out_kind, hipStream_t st) {
   p.tiles_m = (int)ceil_div(p.m, C::BM);
   p.tiles_n = (int)ceil_div(p.n, C::BN);
-  const int64_t blocks = (int64_t)p.tiles_m * p.tiles_n;
-  if (blocks > 0x7fffffff) return CWAC_E_SHAPE;
-  if (out_kind == CWAC_OUT_FP32) return launch_tile_one<C, CWAC_OUT_FP32>(p, (unsigned)blocks, st);
-  if (out_kind == CWAC_OUT_FP16) return launch_tile_one<C, CWAC_OUT_FP16>(p, (unsigned)blocks, st);
-  return launch_tile_one<C, CWAC_OUT_BF16>(p, (unsigned)blocks, st);
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+  if (tiles > 0x3fffffff) return CWAC_E_SHAPE;
+  // as many persistent workgroups as fit the chip (256 compute units); a multiple of 8 keeps a workgroup's tiles on one XCD
+  const int64_t fit = 256 * (160 * 1024 / C::LDS);
+  const unsigned blocks = (unsigned)(tiles < fit ? tiles : fit);
+  if (out_kind == CWAC_OUT_FP32) return launch_tile_one<C, CWAC_OUT_FP32>(p, blocks, st);
+  if (out_kind == CWAC_OUT_FP16) return launch_tile_one<C, CWAC_OUT_FP16>(p, blocks, st);
+  return launch_tile_one<C, CWAC_OUT_BF16>(p, blocks, st);
 }
 
 using Tile256 = Mx4TileCfg<256, 256, 4, 4, 2>;
