@@ -765,8 +765,9 @@ cwac_status qlinear_cwac_forward_fixed_point_ex(const int8_t *x_q, int64_t ldx, 
                                                 const int32_t *shift, const int32_t *offset,
                                                 int8_t *out, int64_t ldo, const cwac_tuning *tuning,
                                                 void *stream);
-/* kernel: CWAC_KERNEL_DIRECT_LDS the tiles (shape CWAC_SHAPE_256_8W: m, n >= 256, CWAC_SHAPE_128_128: m, n >= 128, or the larger that
- * fits), CWAC_KERNEL_SPLIT_K the kernel that splits K over a workgroup's wavefronts; anything else the automatic choice. */
+/* kernel: CWAC_KERNEL_DIRECT_LDS with shape CWAC_SHAPE_256_8W (m, n >= 256), CWAC_SHAPE_128_PAIR (128 x 128 tiles, two workgroups per
+ * compute unit) or CWAC_SHAPE_128_128 (three stages, one workgroup; both m, n >= 128): that tile; CWAC_KERNEL_SPLIT_K: the kernel that splits K
+ * over a workgroup's wavefronts; anything else: the automatic choice. */
 cwac_status qlinear_mx4_cwac_forward_ex(const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales,
                                         const uint8_t *w_codes, int64_t ldw, const uint8_t *w_scales, int64_t m, int32_t n,
                                         int32_t k, const float *mult, const float *fbias, int32_t out_kind, void *out,

@@ -363,25 +363,34 @@ __global__ __launch_bounds__(C::NT) void mx4_tile_kernel(const Mx4Params p) {
   const uint8_t *xg = nullptr, *wg = nullptr, *xsg = nullptr, *wsg = nullptr;
   uint32_t xleft = 0, wleft = 0;
   int xtodo = 0, wtodo = 0;
+  // load i of the stage into ring place buf, and the step to the next stage behind the last one
+  auto load_x = [&](int i, int buf) {
+    if (i < C::LX) {
+      const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(xg), 0, xtodo > 0 ? (int)xleft : 0, 0x00020000);
+      codes_to_lds(d, smem + buf * C::X_BYTES + wave * C::XR * BK + i * 8 * BK, xv[i < C::LX ? i : 0]);
+    } else {
+      const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(xsg), 0, xtodo > 0 ? C::BM * 8 : 0, 0x00020000);
+      words_to_lds(d, smem + C::XS_AT + (buf * C::BM + wave * C::XR + 32 * (i - C::LX)) * 8, xsv + (i - C::LX) * 256);
+    }
+    if (i == C::LX + C::SX - 1) xg += BK, xleft -= BK, xsg += p.m * 8, --xtodo;
+  };
+  auto load_w = [&](int i, int buf) {
+    if (i < C::LW) {
+      const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(wg), 0, wtodo > 0 ? (int)wleft : 0, 0x00020000);
+      codes_to_lds(d, smem + C::W_AT + buf * C::W_BYTES + wave * C::WR * BK + i * 8 * BK, wv[i < C::LW ? i : 0]);
+    } else {
+      const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(wsg), 0, wtodo > 0 ? C::BN * 8 : 0, 0x00020000);
+      words_to_lds(d, smem + C::WS_AT + (buf * C::BN + wave * C::WR + 32 * (i - C::LW)) * 8, wsv + (i - C::LW) * 256);
+    }
+    if (i == C::LW + C::SW - 1) wg += BK, wleft -= BK, wsg += (int64_t)p.n * 8, --wtodo;
+  };
   auto issue_x = [&](int buf) {
-    const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(xg), 0, xtodo > 0 ? (int)xleft : 0, 0x00020000);
-    const __amdgpu_buffer_rsrc_t ds = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(xsg), 0, xtodo > 0 ? C::BM * 8 : 0, 0x00020000);
-    uint8_t *dst = smem + buf * C::X_BYTES + wave * C::XR * BK;
 #pragma unroll
-    for (int i = 0; i < C::LX; ++i) codes_to_lds(d, dst + i * 8 * BK, xv[i]);
-#pragma unroll
-    for (int i = 0; i < C::SX; ++i) words_to_lds(ds, smem + C::XS_AT + (buf * C::BM + wave * C::XR + 32 * i) * 8, xsv + i * 256);
-    xg += BK, xleft -= BK, xsg += p.m * 8, --xtodo;
+    for (int i = 0; i < C::LX + C::SX; ++i) load_x(i, buf);
   };
   auto issue_w = [&](int buf) {
-    const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(wg), 0, wtodo > 0 ? (int)wleft : 0, 0x00020000);
-    const __amdgpu_buffer_rsrc_t ds = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(wsg), 0, wtodo > 0 ? C::BN * 8 : 0, 0x00020000);
-    uint8_t *dst = smem + C::W_AT + buf * C::W_BYTES + wave * C::WR * BK;
 #pragma unroll
-    for (int i = 0; i < C::LW; ++i) codes_to_lds(d, dst + i * 8 * BK, wv[i]);
-#pragma unroll
-    for (int i = 0; i < C::SW; ++i) words_to_lds(ds, smem + C::WS_AT + (buf * C::BN + wave * C::WR + 32 * i) * 8, wsv + i * 256);
-    wg += BK, wleft -= BK, wsg += (int64_t)p.n * 8, --wtodo;
+    for (int i = 0; i < C::LW + C::SW; ++i) load_w(i, buf);
   };
   // a tile's origin, its parameters (the first half of the wavefronts the multipliers, the others the constants), its stage 0
   auto open = [&](int id, int block) {
@@ -406,84 +415,67 @@ __global__ __launch_bounds__(C::NT) void mx4_tile_kernel(const Mx4Params p) {
   const int swz = (l32 >> 1) & 7;
   const int x_row = (wave_m * 32 * TB + l32) * BK, w_row = C::W_AT + (wave_n * 32 * TA + l32) * BK;
   const int xs_row = C::XS_AT + (wave_m * 32 * TB + l32) * 8 + 4 * half, ws_row = C::WS_AT + (wave_n * 32 * TA + l32) * 8 + 4 * half;
-  auto read = [&](int buf, int step, v4i(&fw)[TA], v4i(&fx)[TB]) {
+  // operand i of a step (the channels' first), scale word i of a stage
+  auto read_one = [&](int i, int buf, int step, v4i(&fw)[TA], v4i(&fx)[TB]) {
     const int chunk = ((4 * half + step) ^ swz) << 4;
-#pragma unroll
-    for (int a = 0; a < TA; ++a) fw[a] = *reinterpret_cast<const v4i *>(smem + w_row + chunk + buf * C::W_BYTES + a * 32 * BK);
-#pragma unroll
-    for (int b = 0; b < TB; ++b) fx[b] = *reinterpret_cast<const v4i *>(smem + x_row + chunk + buf * C::X_BYTES + b * 32 * BK);
+    if (i < TA)
+      fw[i < TA ? i : 0] = *reinterpret_cast<const v4i *>(smem + w_row + chunk + buf * C::W_BYTES + i * 32 * BK);
+    else
+      fx[i < TA ? 0 : i - TA] = *reinterpret_cast<const v4i *>(smem + x_row + chunk + buf * C::X_BYTES + (i - TA) * 32 * BK);
   };
-  auto read_scales = [&](int buf, int(&sw)[TA], int(&sx)[TB]) {
-#pragma unroll
-    for (int a = 0; a < TA; ++a) sw[a] = *reinterpret_cast<const int *>(smem + ws_row + buf * C::BN * 8 + a * 256);
-#pragma unroll
-    for (int b = 0; b < TB; ++b) sx[b] = *reinterpret_cast<const int *>(smem + xs_row + buf * C::BM * 8 + b * 256);
+  auto read_scale = [&](int i, int buf, int(&sw)[TA], int(&sx)[TB]) {
+    if (i < TA)
+      sw[i < TA ? i : 0] = *reinterpret_cast<const int *>(smem + ws_row + buf * C::BN * 8 + i * 256);
+    else
+      sx[i < TA ? 0 : i - TA] = *reinterpret_cast<const int *>(smem + xs_row + buf * C::BM * 8 + (i - TA) * 256);
   };
   v16f acc[TA][TB];
   v4i fwA[TA], fxA[TB], fwB[TA], fxB[TB];
   int sw[TA], sx[TB];
-  auto mma = [&](auto step, const v4i(&fw)[TA], const v4i(&fx)[TB]) {
-#pragma unroll
-    for (int a = 0; a < TA; ++a)
-#pragma unroll
-      for (int b = 0; b < TB; ++b)
-        acc[a][b] = mfma32<decltype(step)::value>(fw[a], fx[b], acc[a][b], sw[a], sx[b]);
-  };
-  // one step for the scheduler: the LDS reads behind the first matrix instructions one or two at a time, the loads behind the others
-  auto interleave = [&](int reads, int loads) {
-    constexpr int MM = TA * TB;
-    const int each = (reads + MM - 1) / MM;
-    int r = reads, l = loads;
+  // One step: its matrix instructions in order, behind each of them a share of `reads` (a callable for LDS read i) and of `loads` (for
+  // load i) of n_reads and n_loads.  A load holds up its wavefront while the address unit is busy, so they go out one at a time.
+  auto step = [&](auto tag, const v4i(&fw)[TA], const v4i(&fx)[TB], auto n_reads, auto reads, auto n_loads, auto loads) {
+    constexpr int MM = TA * TB, NR = decltype(n_reads)::value, NL = decltype(n_loads)::value;
 #pragma unroll
     for (int i = 0; i < MM; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      if (r > 0) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        --r;
-        if (each > 1 && r > 0) {
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-          --r;
-        }
-        if (each > 2 && r > 0) {
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-          --r;
-        }
-      }
-      if (l > 0 && i >= MM / 4) {
-        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
-        --l;
-      }
+      const int a = i / TB, b = i % TB;
+      acc[a][b] = mfma32<decltype(tag)::value>(fw[a], fx[b], acc[a][b], sw[a], sx[b]);
+      // the reads behind the first three quarters, the loads spread over all
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+        if (r * (MM * 3 / 4) / NR == i) reads(r);
+#pragma unroll
+      for (int l = 0; l < NL; ++l)
+        if (l * MM / NL == i) loads(l);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_barrier(0);
   };
   using S0 = std::integral_constant<int, 0>;
   using S1 = std::integral_constant<int, 1>;
   using S2 = std::integral_constant<int, 2>;
   using S3 = std::integral_constant<int, 3>;
+  using Operands = std::integral_constant<int, TA + TB>;
   // Stage s in ring place buf.  The loads of stage s + NSTAGE go into the place that this stage leaves, behind its barrier: the
   // tokens' under the last step, the channels' under the first step of the next stage.
-  auto stage_body = [&](int buf) {
-    const int prev = buf == 0 ? NSTAGE - 1 : buf - 1, next = buf == NSTAGE - 1 ? 0 : buf + 1;
-    issue_w(prev);
-    read(buf, 1, fwB, fxB);
-    mma(S0{}, fwA, fxA);
-    interleave(TA + TB, C::LW + C::SW);
-    read(buf, 2, fwA, fxA);
-    mma(S1{}, fwB, fxB);
-    interleave(TA + TB, 0);
-    read(buf, 3, fwB, fxB);
-    mma(S2{}, fwA, fxA);
-    interleave(TA + TB, 0);
+  auto stage_body = [&](int prev, int buf, int next) {
+    auto none = [](int) {};
+    step(S0{}, fwA, fxA, Operands{}, [&](int i) { read_one(i, buf, 1, fwB, fxB); }, std::integral_constant<int, C::LW + C::SW>{},
+         [&](int i) { load_w(i, prev); });
+    step(S1{}, fwB, fxB, Operands{}, [&](int i) { read_one(i, buf, 2, fwA, fxA); }, S0{}, none);
+    step(S2{}, fwA, fxA, Operands{}, [&](int i) { read_one(i, buf, 3, fwB, fxB); }, S0{}, none);
     wait_loads<(NSTAGE - 2) * C::LPS>();  // stage s + 1 has landed
     wait_lds();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    issue_x(buf);
     int nw[TA], nx[TB];
-    read(next, 0, fwA, fxA);
-    read_scales(next, nw, nx);
-    mma(S3{}, fwB, fxB);
-    interleave(2 * (TA + TB), C::LX + C::SX);
+    step(S3{}, fwB, fxB, std::integral_constant<int, 2 * (TA + TB)>{},
+         [&](int i) {
+           if (i < TA + TB)
+             read_one(i, next, 0, fwA, fxA);
+           else
+             read_scale(i - TA - TB, next, nw, nx);
+         },
+         std::integral_constant<int, C::LX + C::SX>{}, [&](int i) { load_x(i, buf); });
 #pragma unroll
     for (int a = 0; a < TA; ++a) sw[a] = nw[a];
 #pragma unroll
@@ -520,14 +512,19 @@ __global__ __launch_bounds__(C::NT) void mx4_tile_kernel(const Mx4Params p) {
       for (int b = 0; b < TB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
-    read(0, 0, fwA, fxA);
-    read_scales(0, sw, sx);
-    int buf = 0;
+#pragma unroll
+    for (int i = 0; i < TA + TB; ++i) {
+      read_one(i, 0, 0, fwA, fxA);
+      read_scale(i, 0, sw, sx);
+    }
+    int prev = NSTAGE - 1, buf = 0, next = 1;
 #pragma unroll 1
     for (int left = stages; left > 0; --left) {
-      stage_body(buf);
-      buf = buf == NSTAGE - 1 ? 0 : buf + 1;
+      stage_body(prev, buf, next);
+      const int after = NSTAGE == 2 ? buf : prev;
+      prev = buf, buf = next, next = after;
     }
+    static_assert(NSTAGE == 2 || NSTAGE == 3, "the rotation above");
     wait_loads<0>();  // the loads past the last stage: their zeros lie where the next tile or the slabs go
     wait_lds();
     __builtin_amdgcn_s_barrier();
@@ -618,8 +615,9 @@ cwac_status launch_tile(Mx4Params p, int out_kind, hipStream_t st) {
   return launch_tile_one<C, CWAC_OUT_BF16>(p, blocks, st);
 }
 
-using Tile256 = Mx4TileCfg<256, 256, 4, 4, 2>;
-using Tile128 = Mx4TileCfg<128, 128, 2, 2, 2>;
+using Tile256 = Mx4TileCfg<256, 256, 4, 4, 2>;      // eight wavefronts of 64 x 128, one workgroup per compute unit
+using Tile128Pair = Mx4TileCfg<128, 128, 2, 2, 2>;  // four of 64 x 64, two workgroups
+using Tile128Deep = Mx4TileCfg<128, 128, 2, 2, 3>;  // one workgroup, three stages: a single round with a long K
 
 }  // namespace
 }  // namespace cwac
@@ -649,14 +647,18 @@ extern "C" cwac_status qlinear_mx4_cwac_forward_ex(const uint8_t *x_codes, int64
   int form = mx4_form(m, n, k);
   if (tune.kernel == CWAC_KERNEL_SPLIT_K) form = mx4_split_form(m, n, k);
   if (tune.kernel == CWAC_KERNEL_DIRECT_LDS) {
-    if (m >= 128 && n >= 128 && (tune.shape == CWAC_SHAPE_128_128 || (tune.shape == CWAC_SHAPE_AUTO && (m < 256 || n < 256)))) form = kMx4Tile128;
-    if (m >= 256 && n >= 256 && (tune.shape == CWAC_SHAPE_256_8W || tune.shape == CWAC_SHAPE_AUTO)) form = kMx4Tile256;
+    if (tune.shape == CWAC_SHAPE_256_8W && m >= 256 && n >= 256) form = kMx4Tile256;
+    if (tune.shape == CWAC_SHAPE_128_PAIR && m >= 128 && n >= 128) form = kMx4Tile128Pair;
+    if (tune.shape == CWAC_SHAPE_128_128 && m >= 128 && n >= 128) form = kMx4Tile128Deep;
   }
   switch (form) {
     case kMx4Tile256: return launch_tile<Tile256>(p, out_kind, st);
-    case kMx4Tile128: return launch_tile<Tile128>(p, out_kind, st);
-    case kMx4Split16: return launch_split<1, 1, 4, 4>(p, out_kind, st);
-    default: return launch_split<2, 2, 4, 2>(p, out_kind, st);
+    case kMx4Tile128Pair: return launch_tile<Tile128Pair>(p, out_kind, st);
+    case kMx4Tile128Deep: return launch_tile<Tile128Deep>(p, out_kind, st);
+    case kMx4Split64: return launch_split<4, 4, 4, 2>(p, out_kind, st);
+    case kMx4Split32: return launch_split<2, 2, 4, 2>(p, out_kind, st);
+    case kMx4Split32x16: return launch_split<2, 1, 4, 3>(p, out_kind, st);
+    default: return launch_split<1, 1, 4, 4>(p, out_kind, st);
   }
 }
 

@@ -125,10 +125,11 @@ def _check(out, xv, wv, mult, fb, t):
 B = P.binding
 # the automatic choice, each tile where it fits, the split-K kernel
 FORMS = [None, B.make_tuning(kernel=B.CWAC_KERNEL_SPLIT_K), B.make_tuning(kernel=B.CWAC_KERNEL_DIRECT_LDS, shape=B.CWAC_SHAPE_128_128),
+         B.make_tuning(kernel=B.CWAC_KERNEL_DIRECT_LDS, shape=B.CWAC_SHAPE_128_PAIR),
          B.make_tuning(kernel=B.CWAC_KERNEL_DIRECT_LDS, shape=B.CWAC_SHAPE_256_8W)]
 SIZES = [(1, 1, 32), (1, 4096, 4096), (2, 17, 64), (5, 100, 96), (16, 256, 256), (17, 33, 288), (31, 1000, 5504), (64, 320, 1024),
          (127, 129, 384), (128, 257, 2016), (255, 255, 160), (256, 256, 256), (257, 511, 544), (300, 2049, 1088),
-         (513, 768, 768), (700, 4100, 224), (1030, 1024, 4096), (2049, 640, 1312)]
+         (513, 768, 768), (700, 4100, 224), (1030, 1024, 4096), (2049, 640, 1312), (249, 4090, 4192), (9, 9000, 352), (30, 500, 800)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
@@ -179,6 +180,27 @@ def test_bytes_between_rows_do_not_enter(m, n, k):
         P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, None, None, out, tuning=tuning)
         assert (out[3] == 0).all()
         _check(out, _values(xc, xs, k), _values(wc, ws, k), None, None, "f32")
+
+
+@pytest.mark.parametrize("shape", [B.CWAC_SHAPE_256_8W, B.CWAC_SHAPE_128_PAIR, B.CWAC_SHAPE_128_128])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_persistent_tiles_in_several_rounds(shape, t):
+    """More tiles than workgroups, ragged edges, K shorter and longer than the ring: every tile begins with the ring, the parameter
+    blocks and the slabs as the one before left them."""
+    tuning = B.make_tuning(kernel=B.CWAC_KERNEL_DIRECT_LDS, shape=shape)
+    for m, n, k in ((4500, 4600, 224), (4100, 4500, 480), (2900, 8200, 1120)):
+        x, w, mult, fb = _layer(m, n, k, 3)
+        xc, xs = _quantize(x)
+        wc, ws = _quantize(w)
+        xv, wv = _values(xc, xs, k), _values(wc, ws, k)
+        out = torch.full((m, n), float("nan"), dtype=TYPES[t], device=DEV)
+        P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, mult, fb, out, tuning=tuning)
+        _check(out, xv, wv, mult, fb, t)
+        odd = torch.full((m, n + 3), 7.0, dtype=TYPES[t], device=DEV)[:, :n]          # element-wise stores
+        P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, mult, None, odd, tuning=tuning)
+        _check(odd, xv, wv, mult, None, t)
+        P.qlinear_mx4_cwac_forward(xc, xs, wc, ws, None, fb, out, tuning=tuning)
+        _check(out, xv, wv, None, fb, t)
 
 
 def test_extreme_scales():
