@@ -15,47 +15,71 @@ namespace {
 
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+// STREAM: past the caches, for values that would only push the codes out of them.
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load16(const V *p) {
+  if constexpr (STREAM)
+    return __builtin_nontemporal_load(p);
+  else
+    return *p;
+}
+
+template <bool STREAM, typename V>
+__device__ __forceinline__ void store16(V *p, V v) {
+  if constexpr (STREAM)
+    __builtin_nontemporal_store(v, p);
+  else
+    *p = v;
+}
 
 // Eight consecutive values as they lie in memory, and as fp32.
 template <int TYPE>
 struct Eight;
 template <>
 struct Eight<CWAC_OUT_FP32> {
-  float4 a, b;
+  v4f a, b;
   static constexpr int SIZE = 4;
+  template <bool STREAM>
   __device__ __forceinline__ void load(const char *p) {
-    a = reinterpret_cast<const float4 *>(p)[0];
-    b = reinterpret_cast<const float4 *>(p)[1];
+    a = load16<STREAM>(reinterpret_cast<const v4f *>(p));
+    b = load16<STREAM>(reinterpret_cast<const v4f *>(p) + 1);
   }
   __device__ __forceinline__ void get(float (&v)[8]) const {
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[i + 4] = b[i];
   }
+  template <bool STREAM>
   __device__ static __forceinline__ void store(char *p, const float (&v)[8]) {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    store16<STREAM>(reinterpret_cast<v4f *>(p), v4f{v[0], v[1], v[2], v[3]});
+    store16<STREAM>(reinterpret_cast<v4f *>(p) + 1, v4f{v[4], v[5], v[6], v[7]});
   }
 };
 template <>
 struct Eight<CWAC_OUT_FP16> {
   h8 a;
   static constexpr int SIZE = 2;
-  __device__ __forceinline__ void load(const char *p) { a = *reinterpret_cast<const h8 *>(p); }
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const char *p) { a = load16<STREAM>(reinterpret_cast<const h8 *>(p)); }
   __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
   }
+  template <bool STREAM>
   __device__ static __forceinline__ void store(char *p, const float (&v)[8]) {
     h8 r;
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = (_Float16)v[i];
-    *reinterpret_cast<h8 *>(p) = r;
+    store16<STREAM>(reinterpret_cast<h8 *>(p), r);
   }
 };
 template <>
 struct Eight<CWAC_OUT_BF16> {
   u4 a;
   static constexpr int SIZE = 2;
-  __device__ __forceinline__ void load(const char *p) { a = *reinterpret_cast<const u4 *>(p); }
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const char *p) { a = load16<STREAM>(reinterpret_cast<const u4 *>(p)); }
   __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -64,11 +88,12 @@ struct Eight<CWAC_OUT_BF16> {
     }
   }
   // the numbers of a block have two significant bits: their upper half is all of them (2^-128, the smallest, included)
+  template <bool STREAM>
   __device__ static __forceinline__ void store(char *p, const float (&v)[8]) {
     u4 r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
-    *reinterpret_cast<u4 *>(p) = r;
+    store16<STREAM>(reinterpret_cast<u4 *>(p), r);
   }
 };
 
@@ -81,9 +106,9 @@ __device__ __forceinline__ uint32_t dpp(uint32_t v) {
 }
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// ROWS consecutive rows x 512 values per wavefront and step: their loads are in flight together, and a panel's scale
-// bytes of the rows lie side by side.
-template <int TYPE, int ROWS>
+// ROWS consecutive rows x 512 values per wavefront and step: their loads are in flight together, and the scale bytes of a panel's
+// rows, which lie side by side, go out in one store.
+template <int TYPE, int ROWS, bool STREAM>
 __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(const char *__restrict__ x, int64_t ldx, int64_t rows, int k,
                                                                 uint8_t *__restrict__ codes, int64_t ldc,
                                                                 uint8_t *__restrict__ scales, int chunks, int64_t tasks) {
@@ -98,10 +123,12 @@ __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(const char *__re
     E raw[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
-      if (in && r < n) raw[r].load(x + ((r0 + r) * ldx + col) * E::SIZE);
+      if (in && r < n) raw[r].template load<STREAM>(x + ((r0 + r) * ldx + col) * E::SIZE);
+    uint32_t bytes[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      if (r >= n) break;
+      bytes[r] = 0;
+      if (r >= n) continue;
       float v[8];
       uint32_t top = 0;
       if (in) {
@@ -127,56 +154,76 @@ __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(const char *__re
       if (code == 255u) word = 0;
       if (in) *reinterpret_cast<uint32_t *>(codes + (r0 + r) * ldc + col / 2) = word;
       // four blocks' bytes to a word, in every lane of a row of 16
-      uint32_t bytes = (in ? code : 0u) << (8 * ((lane >> 2) & 3));
-      bytes |= dpp<0x124>(bytes);
-      bytes |= dpp<0x128>(bytes);
-      const int panel = chunk * (kChunk / kMx4Panel) + (lane >> 5);
-      if ((lane & 15) == 0 && panel * kMx4Panel < k)
-        *reinterpret_cast<uint32_t *>(scales + ((int64_t)panel * rows + r0 + r) * 8 + ((lane >> 4) & 1) * 4) = bytes;
+      uint32_t b = (in ? code : 0u) << (8 * ((lane >> 2) & 3));
+      b |= dpp<0x124>(b);
+      bytes[r] = b | dpp<0x128>(b);
     }
+    // lane r of 16 stores row r's word
+    uint32_t mine = bytes[0];
+#pragma unroll
+    for (int r = 1; r < ROWS; ++r) mine = (lane & 15) == r ? bytes[r] : mine;
+    const int panel = chunk * (kChunk / kMx4Panel) + (lane >> 5);
+    if ((lane & 15) < n && panel * kMx4Panel < k)
+      *reinterpret_cast<uint32_t *>(scales + ((int64_t)panel * rows + r0 + (lane & 15)) * 8 + ((lane >> 4) & 1) * 4) = mine;
   }
 }
 
-template <int TYPE>
+template <int TYPE, int ROWS, bool STREAM>
 __global__ __launch_bounds__(kThreads) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes, int64_t ldc,
                                                                   const uint8_t *__restrict__ scales, int64_t rows, int k,
                                                                   char *__restrict__ out, int64_t ldo, int chunks, int64_t tasks) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   for (int64_t task = (int64_t)blockIdx.x * (kThreads / 64) + wave; task < tasks; task += (int64_t)gridDim.x * (kThreads / 64)) {
-    const int64_t r = task / chunks;
+    const int64_t r0 = task / chunks * ROWS;
     const int col = (int)(task % chunks) * kChunk + lane * 8;
     if (col >= k) continue;
-    const uint32_t word = *reinterpret_cast<const uint32_t *>(codes + r * ldc + col / 2);
-    const uint32_t code = scales[((int64_t)(col / kMx4Panel) * rows + r) * 8 + (col % kMx4Panel) / kMx4Block];
-    const float s = code == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(code ? code << 23 : 0x00400000u);
-    float v[8];
+    const int n = rows - r0 < ROWS ? (int)(rows - r0) : ROWS;
+    uint32_t words[ROWS], scale[ROWS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      // magnitudes 2 m = 0, 1, 2, 3, 4, 6, 8, 12, a nibble each
-      const uint32_t c = (word >> (4 * i)) & 15u;
-      const float m = 0.5f * (float)((0xc8643210u >> (4 * (c & 7u))) & 15u);
-      v[i] = (c & 8u ? -m : m) * s;
+    for (int r = 0; r < ROWS; ++r)
+      if (r < n) {
+        words[r] = *reinterpret_cast<const uint32_t *>(codes + (r0 + r) * ldc + col / 2);
+        scale[r] = scales[((int64_t)(col / kMx4Panel) * rows + r0 + r) * 8 + (col % kMx4Panel) / kMx4Block];
+      }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (r >= n) break;
+      const uint32_t word = words[r], code = scale[r];
+      const float s = code == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(code ? code << 23 : 0x00400000u);
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // magnitudes 2 m = 0, 1, 2, 3, 4, 6, 8, 12, a nibble each
+        const uint32_t c = (word >> (4 * i)) & 15u;
+        const float m = 0.5f * (float)((0xc8643210u >> (4 * (c & 7u))) & 15u);
+        v[i] = (c & 8u ? -m : m) * s;
+      }
+      Eight<TYPE>::template store<STREAM>(out + ((r0 + r) * ldo + col) * Eight<TYPE>::SIZE, v);
     }
-    Eight<TYPE>::store(out + (r * ldo + col) * Eight<TYPE>::SIZE, v);
   }
 }
 
 constexpr int64_t kMaxBlocks = 1 << 20;
+// values of half the last-level cache and more would leave nothing of the codes in it
+constexpr int64_t kStreamBytes = (int64_t)128 << 20;
 
 template <int TYPE>
 cwac_status launch_quantize(const void *x, int64_t ldx, int64_t rows, int k, uint8_t *codes, int64_t ldc, uint8_t *scales, hipStream_t st) {
   const int chunks = (int)ceil_div(k, kChunk);
   // eight rows to a wavefront once that still leaves wavefronts for every SIMD; single rows below
   const bool many = rows * chunks >= 8 * 4096;
+  const bool stream = many && rows * k * Eight<TYPE>::SIZE >= kStreamBytes;
   const int64_t tasks = (many ? ceil_div(rows, 8) : rows) * chunks;
   const int64_t blocks = ceil_div(tasks, kThreads / 64);
   const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks));
   const char *xp = static_cast<const char *>(x);
-  if (many)
-    mx4_quantize_kernel<TYPE, 8><<<grid, kThreads, 0, st>>>(xp, ldx, rows, k, codes, ldc, scales, chunks, tasks);
+  if (stream)
+    mx4_quantize_kernel<TYPE, 8, true><<<grid, kThreads, 0, st>>>(xp, ldx, rows, k, codes, ldc, scales, chunks, tasks);
+  else if (many)
+    mx4_quantize_kernel<TYPE, 8, false><<<grid, kThreads, 0, st>>>(xp, ldx, rows, k, codes, ldc, scales, chunks, tasks);
   else
-    mx4_quantize_kernel<TYPE, 1><<<grid, kThreads, 0, st>>>(xp, ldx, rows, k, codes, ldc, scales, chunks, tasks);
+    mx4_quantize_kernel<TYPE, 1, false><<<grid, kThreads, 0, st>>>(xp, ldx, rows, k, codes, ldc, scales, chunks, tasks);
   return launch_status();
 }
 
@@ -184,9 +231,16 @@ template <int TYPE>
 cwac_status launch_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scales, int64_t rows, int k, void *out, int64_t ldo,
                               hipStream_t st) {
   const int chunks = (int)ceil_div(k, kChunk);
-  const int64_t tasks = rows * chunks, blocks = ceil_div(tasks, kThreads / 64);
+  const bool many = rows * chunks >= 8 * 4096;
+  const int64_t tasks = (many ? ceil_div(rows, 8) : rows) * chunks, blocks = ceil_div(tasks, kThreads / 64);
   const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks));
-  mx4_dequantize_kernel<TYPE><<<grid, kThreads, 0, st>>>(codes, ldc, scales, rows, k, static_cast<char *>(out), ldo, chunks, tasks);
+  const bool stream = many && rows * k * Eight<TYPE>::SIZE >= kStreamBytes;
+  if (stream)
+    mx4_dequantize_kernel<TYPE, 8, true><<<grid, kThreads, 0, st>>>(codes, ldc, scales, rows, k, static_cast<char *>(out), ldo, chunks, tasks);
+  else if (many)
+    mx4_dequantize_kernel<TYPE, 8, false><<<grid, kThreads, 0, st>>>(codes, ldc, scales, rows, k, static_cast<char *>(out), ldo, chunks, tasks);
+  else
+    mx4_dequantize_kernel<TYPE, 1, false><<<grid, kThreads, 0, st>>>(codes, ldc, scales, rows, k, static_cast<char *>(out), ldo, chunks, tasks);
   return launch_status();
 }
 
