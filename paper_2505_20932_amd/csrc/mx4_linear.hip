@@ -572,8 +572,12 @@ __global__ __launch_bounds__(C::NT) void mx4_tile_kernel(const Mx4Params p) {
 #pragma unroll
           for (int i = 0; i < 32 / RPS; ++i) {
             const int row = i * RPS + lane / LPR;
-            *reinterpret_cast<v4i *>(o + row * p.ldo + (lane % LPR) * (16 / ES)) =
-                *reinterpret_cast<const v4i *>(slab + row * ROW + (((lane % LPR) ^ (row & (LPR - 1))) << 4));
+            const v4i v = *reinterpret_cast<const v4i *>(slab + row * ROW + (((lane % LPR) ^ (row & (LPR - 1))) << 4));
+            v4i *dst = reinterpret_cast<v4i *>(o + row * p.ldo + (lane % LPR) * (16 / ES));
+            if constexpr (C::BM == 256)  // these outputs are larger than the L2s
+              __builtin_nontemporal_store(v, dst);
+            else
+              *dst = v;
           }
         } else {  // whole wavefronts over consecutive elements of a row
           constexpr int EPR = ROW / ES, LANES = EPR < 64 ? EPR : 64;

@@ -18,7 +18,6 @@ enum { kMx4Split16 = 1, kMx4Split32x16, kMx4Split32, kMx4Split64, kMx4Tile128Dee
 //   256 x 4096 x 4096                 9.9        8.7       10.9       14.6      25.0
 //   601 x 4096 x 4096                19.9       22.2       11.8       15.3      25.2
 //   256 x 4096 x 11008               23.6       17.7       29.5       41.0      69.7
-//   1024 x 768 x 3072                 7.3        7.8        9.6       12.6      21.2
 //   601 x 2304 x 768                  7.6        9.2        6.6        6.8      12.1
 //   2048 x 4096 x 4096               67         62         28.8       25.4      35.5
 //   4096 x 4096 x 4096              125        122         54.7       47.2      43.4
