@@ -538,7 +538,7 @@ cwac_status llm_kv_assign_pages(const int32_t *old_lens, const int32_t *new_lens
  *   k, v    device [tokens, kv_heads * head_dim] of `type` (CWAC_OUT_FP16 or CWAC_OUT_BF16), pitches ldk, ldv elements (they may be columns of
  *           the qkv layer's output); 16-byte aligned, pitches % 8 == 0; a 16-bit cache is of the same type
  *   slots   device int64 [tokens]; a slot that is named twice holds either token's values, or a mixture
- *   tokens >= 0 (0 is a no-op) */
+ *   0 <= tokens < 2^31 (0 is a no-op) */
 cwac_status llm_kv_append(const void *k, int64_t ldk, const void *v, int64_t ldv, int32_t type, const int64_t *slots,
                           int64_t tokens, int32_t kv_heads, int32_t head_dim, void *k_cache, void *v_cache,
                           int32_t cache_type, float *k_scales, float *v_scales, int32_t n_pages, int32_t page,
@@ -554,7 +554,9 @@ cwac_status llm_kv_append(const void *k, int64_t ldk, const void *v, int64_t ldv
  *   a 16-bit cache is of q's type; 1 <= batch <= 65535, q_heads % kv_heads == 0, kv_heads <= 1024
  *   workspace  device, llm_paged_attention_workspace(...) bytes, 16-byte aligned, for calls in order on one stream: it holds the parts
  *              of split lengths between the call's two launches (calls that may overlap need one each)
- * Logits, maximum, sum and output are accumulated in fp32, a weight meets its value as the sum of two terms of `type`.
+ * Logits, maximum, sum and output are accumulated in fp32.  Over a 16-bit cache a weight meets its value as the sum of two terms of
+ * `type`, over an 8-bit cache as one binary16 number; there bfloat16 queries enter as binary16 numbers relative to a power of two
+ * near their head's largest value.
  * How a length is split follows from batch, heads, table_cols * page and window alone: a request's result does not depend on the
  * other requests' lengths or contents. */
 size_t llm_paged_attention_workspace(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim,

@@ -621,9 +621,7 @@ extern "C" cwac_status llm_paged_attention(const void *q, int64_t ldq, int32_t t
       !aligned(out, 8) || ldo % 4 != 0 || (int8 && (!aligned(k_scales, 4) || !aligned(v_scales, 4))))
     return CWAC_E_ALIGN;
   PagedParams p{};
-  // a window's tokens lie in at most one tile more than its own number
-  int64_t tokens = (int64_t)table_cols * page;
-  if (window > 0 && window + kPagedTile - 1 < tokens) tokens = window + kPagedTile - 1;
+  const int64_t tokens = paged_span((int64_t)table_cols * page, window);
   p.splits = paged_splits(batch, q_heads, kv_heads, tokens);
   const int64_t chunk = paged_chunk(tokens, p.splits);
   p.splits = (int)ceil_div(tokens, chunk);

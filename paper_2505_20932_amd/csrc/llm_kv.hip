@@ -237,9 +237,9 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(const AppendP
 
 template <bool INT8, bool BF16>
 cwac_status launch_append(const AppendParams &p, hipStream_t st) {
-  // Four tokens to a thread once single ones fill the chip with threads several times.  What a prefill writes is far larger than the
-  // L2s and goes past them: 16384 tokens of 8 heads of 128, bf16, 30.4 -> 25.1 us (5.3 TB/s), 4096 tokens 7.5 -> 6.6.  A decoding
-  // step's few tokens stay, for the attention behind it.
+  // Four tokens to a thread once single ones fill the chip with threads several times.  What those write goes past the caches:
+  // 16384 tokens of 8 heads of 128, bf16, 30.4 -> 25.2 us (5.3 TB/s), 4096 tokens (16 MB) 7.5 -> 6.7.  A decoding step's few tokens
+  // stay, for the attention behind it.
   const bool many = p.tokens * p.units >= 4 * 262144;
   const int64_t steps = many ? ceil_div(p.tokens, 4) : p.tokens;
   const int64_t blocks = ceil_div(steps * p.units, kAppendThreads);
@@ -317,7 +317,7 @@ extern "C" cwac_status llm_kv_append(const void *k, int64_t ldk, const void *v, 
   if (type != CWAC_OUT_FP16 && type != CWAC_OUT_BF16) return CWAC_E_MODE;
   const bool int8 = cache_type == CWAC_OUT_INT8;
   if (!int8 && cache_type != type) return CWAC_E_MODE;
-  if (tokens < 0 || kv_heads < 1 || kv_heads > 1024 || (head_dim != 64 && head_dim != 128 && head_dim != 256) || n_pages < 1 ||
+  if (tokens < 0 || tokens > 0x7fffffff || kv_heads < 1 || kv_heads > 1024 || (head_dim != 64 && head_dim != 128 && head_dim != 256) || n_pages < 1 ||
       !page_shift(page, &p.shift) || ldk < (int64_t)kv_heads * head_dim || ldv < (int64_t)kv_heads * head_dim)
     return CWAC_E_SHAPE;
   if (tokens == 0) return CWAC_OK;

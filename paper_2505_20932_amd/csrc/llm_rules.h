@@ -11,6 +11,12 @@ constexpr int kPagedWaves = 4;    // wavefronts of a workgroup: they take turns 
 constexpr int kPagedHeads = 16;   // query heads of one key head that share a workgroup: the columns of the matrix instruction
 constexpr int kPagedMaxSplits = 128;
 
+// Positions that a request's visible tokens can take: a window's lie in at most one tile more than its own number.
+inline int64_t paged_span(int64_t cap, int window) {
+  const int64_t n = (int64_t)window + kPagedTile - 1;
+  return window > 0 && n < cap ? n : cap;
+}
+
 // Splits of `tokens` positions.  A workgroup has a fixed cost of 1.6 us (its first loads, the join), so splits are long, 1024
 // tokens, where there are enough of them - at most 4096 workgroups, for requests of uneven lengths - and shorter only to fill the chip
 // with workgroups (two per compute unit, twice), down to a turn of the wavefronts.  Measured in us with at most 1024 / 2048 / 4096 workgroups and
