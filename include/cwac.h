@@ -532,8 +532,9 @@ cwac_status llm_kv_assign_pages(const int32_t *old_lens, const int32_t *new_lens
                                 int32_t *token_start, int32_t *seq_lens, int32_t *n_left, void *stream);
 
 /* New keys and values into the cache: row i of k and v goes to slot slots[i]; rows with a slot outside
- * [0, n_pages * page) are left out.  16-bit caches take the values as they are; an 8-bit cache stores round(x / s) with
- * s = max |x| / 127 over the head's values of the token (floored at FLT_MIN * 256: cwac_quantize_rows_sym); a token's head that
+ * [0, n_pages * page) are left out.  16-bit caches take the values as they are; an 8-bit cache stores round(x / s) (fp32, ties to
+ * even) with s = max |x| * r over the head's values of the token, r = 1 / 127 rounded to fp32 (floored at FLT_MIN * 256; it may
+ * differ from cwac_quantize_rows_sym's quotient in the last place, and so may a code midway between two); a token's head that
  * holds a NaN or an infinity is stored as NaN (scale NaN, codes 0).
  *   k, v    device [tokens, kv_heads * head_dim] of `type` (CWAC_OUT_FP16 or CWAC_OUT_BF16), pitches ldk, ldv elements (they may be columns of
  *           the qkv layer's output); 16-byte aligned, pitches % 8 == 0; a 16-bit cache is of the same type
@@ -554,9 +555,8 @@ cwac_status llm_kv_append(const void *k, int64_t ldk, const void *v, int64_t ldv
  *   a 16-bit cache is of q's type; 1 <= batch <= 65535, q_heads % kv_heads == 0, kv_heads <= 1024
  *   workspace  device, llm_paged_attention_workspace(...) bytes, 16-byte aligned, for calls in order on one stream: it holds the parts
  *              of split lengths between the call's two launches (calls that may overlap need one each)
- * Logits, maximum, sum and output are accumulated in fp32.  Over a 16-bit cache a weight meets its value as the sum of two terms of
- * `type`, over an 8-bit cache as one binary16 number; there bfloat16 queries enter as binary16 numbers relative to a power of two
- * near their head's largest value.
+ * Logits, maximum, sum and output are accumulated in fp32, a weight meets its value as the sum of two terms: of `type`, over an 8-bit
+ * cache of binary16; there bfloat16 queries enter as binary16 numbers relative to a power of two near their head's largest value.
  * How a length is split follows from batch, heads, table_cols * page and window alone: a request's result does not depend on the
  * other requests' lengths or contents. */
 size_t llm_paged_attention_workspace(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim,

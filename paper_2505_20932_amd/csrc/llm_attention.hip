@@ -16,9 +16,10 @@
 //   * an 8-bit cache is widened to binary16 in registers (exact); the keys' scales multiply the logits, the values' scales the
 //     weights, relative to a running power of two so that small ones lose nothing.  bfloat16 queries become binary16 relative to
 //     the head's largest one (what falls below 2^-25 of that is lost).
-// Over 16-bit caches weights meet the values as a sum of two numbers of the values' type (rounded at 2^-22 or 2^-17 of a weight): two
-// matrix instructions instead of one, which nothing waits for.  Over 8-bit caches, where the vector ALU sets the pace, as one
-// binary16 number (2^-12).  Maximum, sum and output are fp32.
+// Weights meet the values as a sum of two numbers of the matrix instruction's type (off by 2^-20 of a weight at most in binary16, the two
+// cut off rather than rounded, which is one instruction for a pair; 2^-17 in bfloat16).  One binary16 number would be off by 2^-11 and lets
+// int8 caches' outputs be 1.7 times as far from the exact ones; the second one's matrix instructions wait for nothing (five requests
+// of 30011 to 131072 tokens 173.8 us either way).  Maximum, sum and output are fp32.
 // Tokens outside [lo, len), and those of a page whose number is not one, get weight 0, and what the cache holds there is
 // replaced by 0, NaN included.
 #include <type_traits>
@@ -450,9 +451,15 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
     u4 hi, lo;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint16_t a0 = narrow<MB>(w[2 * i]), a1 = narrow<MB>(w[2 * i + 1]);
-      hi[i] = (uint32_t)a0 | (uint32_t)a1 << 16;
-      if (!I8) lo[i] = (uint32_t)narrow<MB>(w[2 * i] - wide<MB>(a0)) | (uint32_t)narrow<MB>(w[2 * i + 1] - wide<MB>(a1)) << 16;
+      if constexpr (MB) {
+        const uint16_t a0 = narrow<MB>(w[2 * i]), a1 = narrow<MB>(w[2 * i + 1]);
+        hi[i] = (uint32_t)a0 | (uint32_t)a1 << 16;
+        lo[i] = (uint32_t)narrow<MB>(w[2 * i] - wide<MB>(a0)) | (uint32_t)narrow<MB>(w[2 * i + 1] - wide<MB>(a1)) << 16;
+      } else {
+        const auto a = __builtin_amdgcn_cvt_pkrtz(w[2 * i], w[2 * i + 1]);
+        hi[i] = __builtin_bit_cast(uint32_t, a);
+        lo[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(w[2 * i] - (float)a[0], w[2 * i + 1] - (float)a[1]));
+      }
     }
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {  // after the first tiles a maximum seldom moves
 #pragma unroll
@@ -462,7 +469,7 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
     for (int t = 0; t < DT; ++t) {
       const u4 val = I8 ? widen(fv[t][0], fv[t][1]) : fv[t];
       acc[t] = mma<MB>(val, hi, acc[t]);
-      if (!I8) acc[t] = mma<MB>(val, lo, acc[t]);
+      acc[t] = mma<MB>(val, lo, acc[t]);
     }
     settle();
     idA = nextA;

@@ -169,8 +169,8 @@ def _run(q, k, v, ks, vs, table, lens, scale, window, page):
 
 
 def _check(out, q, k, v, ks, vs, table, lens, scale, window, t):
-    """Bound of the error: the output's rounding; a weight's (binary16: half a step, and half its smallest step next to the largest
-    weight 1; two bfloat16 terms: 2^-16); the logits' fp32 sums, products and exponential, which enter a weight
+    """Bound of the error: the output's rounding; a weight's (two binary16 terms that are cut off: 2^-10 of 2^-10, and binary16's smallest
+    step next to the largest weight 1; two bfloat16 terms: 2^-16); the logits' fp32 sums, products and exponential, which enter a weight
     relatively and both sums; fp32 sums over the tokens.  All of them times sum w |v|, the smallest step times max |v|.
     8-bit caches: weights are binary16 for either type, and bfloat16 queries become binary16 relative to 2^e <= 2 max |q|, each off by
     at most half its smallest step, 2^-25 * 2^e."""
@@ -178,7 +178,7 @@ def _check(out, q, k, v, ks, vs, table, lens, scale, window, t):
     d = q.shape[2]
     want, mag, seen, qk = orc.attention(q.double().cpu().numpy(), kn, vn, table.cpu().numpy(), lens.cpu().numpy(), scale, window,
                                         q.shape[1] // k.shape[1])
-    weight = 2.0 ** -11 if t == "f16" or k.dtype == torch.int8 else 2.0 ** -16
+    weight = 2.0 ** -20 if t == "f16" or k.dtype == torch.int8 else 2.0 ** -16
     logit = (d / 16 + 8) * 2.0 ** -23 * (qk + 1.0)
     half = t == "f16" or k.dtype == torch.int8
     if t == "bf16" and half:
