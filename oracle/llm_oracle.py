@@ -36,7 +36,7 @@ def rows_sym(x):
     x = np.asarray(x, dtype=np.float32)
     top = np.abs(x).max(axis=-1)
     ok = np.isfinite(top) & np.isfinite(x).all(axis=-1)
-    s = np.where(ok, np.maximum(np.where(ok, top, 0).astype(np.float32) / np.float32(127), TINY), np.float32(np.nan)).astype(np.float32)
+    s = np.where(ok, np.maximum(np.where(ok, top, 0).astype(np.float32) * np.float32(1 / 127), TINY), np.float32(np.nan)).astype(np.float32)
     with np.errstate(invalid="ignore"):
         c = np.clip(np.rint(x / s[..., None]), -127, 127)
     return np.where(ok[..., None], c, 0).astype(np.int8), s

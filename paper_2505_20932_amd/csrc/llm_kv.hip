@@ -136,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void kv_assign_kernel(const AssignParams 
 // ------------------------------------------------------------------------------------------
 // New keys and values into the cache.  Bound: HBM, each value read and written once.  A thread moves 16 bytes (eight values) of
 // TOK tokens; neighbouring lanes take neighbouring pieces of a token's row, which are contiguous within a head on both sides.
-// An 8-bit cache keeps code = round(x / s), s = max |x| / 127 over the token's head: its head_dim / 8 lanes lie in one group of
+// An 8-bit cache keeps code = round(x / s), s = max |x| * (1 / 127) over the token's head: its head_dim / 8 lanes lie in one group of
 // 8, 16 or 32 and take the maximum by cross-lane steps.
 // ------------------------------------------------------------------------------------------
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(const AppendP
         top = other > top ? other : top;
       }
       const bool finite = top < 0x7f800000u;
-      const float s = finite ? fmaxf(__fdiv_rn(__uint_as_float(top), 127.0f), 0x1p-118f) : __uint_as_float(0x7fc00000u);
+      const float s = finite ? fmaxf(__uint_as_float(top) * (1.0f / 127.0f), 0x1p-118f) : __uint_as_float(0x7fc00000u);
       uint32_t w[2] = {0, 0};
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
