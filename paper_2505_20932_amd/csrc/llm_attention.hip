@@ -3,9 +3,10 @@
 //
 // Bound: HBM - every visible key and value is read once, 2 to 32 operations per byte (heads that share a key head share
 // the read); 61 requests of up to 8190 tokens, 8 key heads of 128, bf16: 185 us = 5.5 TB/s, int8 with 5 of up to 131072: 165 us, 5.2 TB/s.  So the kernel is a stream:
-//   * a workgroup takes one request, one key head (up to 16 query heads) and a part of the length; its four wavefronts
-//     take turns over tiles of 32 tokens, each on its own: running maximum, sum and output per wavefront, joined through LDS at the
-//     end and, where the length is split, by a second small kernel through the workspace (fixed order, no atomics);
+//   * a workgroup takes one request, one key head (up to 16 query heads) and a part of the length; its four wavefronts (eight where
+//     they take a short length whole) take turns over tiles of 32 tokens, each on its own: running maximum, sum and output per
+//     wavefront, joined through LDS at the end and, where the length is split, by a second small kernel through the workspace (fixed
+//     order, no atomics);
 //   * keys and values go global -> LDS directly (no registers held while they travel), per 16 tokens one contiguous piece of a page; the
 //     buffers of keys and of values are refilled in turn, so one of the two is always in flight, and two workgroups share a
 //     compute unit;
@@ -54,6 +55,7 @@ struct PagedParams {
   int negate;        // scale < 0: the queries change sign
   int batch, q_heads, kv_heads, group, tiles, shift, cols, n_pages, window;
   int splits, split_tiles;
+  int wide;          // kPagedWide wavefronts and no split
 };
 
 // The part of a request's length that is seen, in tiles, and how many splits it takes.
@@ -70,7 +72,8 @@ struct Span {
   }
 };
 
-template <int D, bool I8>
+// W wavefronts to a workgroup
+template <int D, bool I8, int W>
 struct PagedCfg {
   static constexpr int RB = D * (I8 ? 1 : 2);      // bytes of a row
   static constexpr int CPR = RB / 16;              // 16-byte chunks of it
@@ -80,8 +83,8 @@ struct PagedCfg {
   static constexpr int WAVE = 2 * TILE + 2 * SCALES;  // a wavefront's keys, values and their scales
   static constexpr int LOADS = 2 * LB + (I8 ? 1 : 0);
   static constexpr int SLAB = (D + 4) * 4;            // a head's partial output, 16 bytes apart from the next bank round
-  static constexpr int JOIN = kPagedWaves * (kPagedHeads * SLAB + kPagedHeads * 8);
-  static constexpr int LDS = kPagedWaves * WAVE > JOIN ? kPagedWaves * WAVE : JOIN;
+  static constexpr int JOIN = W * (kPagedHeads * SLAB + kPagedHeads * 8);
+  static constexpr int LDS = W * WAVE > JOIN ? W * WAVE : JOIN;
   // chunk c of row r lies at position c ^ swz(r): 16 rows of one chunk, and 4 x 32-byte pieces of 16 rows, hit distinct banks
   static constexpr int PER = RB >= 256 ? 1 : 256 / RB;  // rows of a bank round
   __host__ __device__ static constexpr int swz(int r) { return (r / PER) & (CPR < 16 ? CPR - 1 : 15); }
@@ -186,9 +189,9 @@ __device__ __forceinline__ float wide(uint16_t h) {
 }
 
 // BF16: the type of the queries and the output, and of a 16-bit cache.
-template <int D, bool BF16, bool I8>
-__global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const PagedParams p) {
-  using C = PagedCfg<D, I8>;
+template <int D, bool BF16, bool I8, int W>
+__global__ __launch_bounds__(64 * W) void paged_attention_kernel(const PagedParams p) {
+  using C = PagedCfg<D, I8, W>;
   constexpr int KS = D / 32, DT = D / 16;
   constexpr bool MB = BF16 && !I8;  // the matrix instructions' type
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -200,7 +203,7 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   auto page_of = [&](int first_tile, int j) {
-    const int64_t col = (int64_t)(2 * (first_tile + wave + kPagedWaves * (j + (lane >> 1))) + (lane & 1)) >> (p.shift - 4);
+    const int64_t col = (int64_t)(2 * (first_tile + wave + W * (j + (lane >> 1))) + (lane & 1)) >> (p.shift - 4);
     return col < p.cols ? p.table[b * p.ldt + col] : -1;
   };
   int raw = p.window == 0 ? page_of(split * p.split_tiles, 0) : -1;
@@ -210,19 +213,19 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
   uint16_t *out = reinterpret_cast<uint16_t *>(p.out) + b * p.ldo + (int64_t)head0 * D;
   if (split >= span.used) {
     if (split == 0)  // nothing is seen
-      for (int i = tid; i < heads * (D / 4); i += 64 * kPagedWaves) reinterpret_cast<u2 *>(out)[i] = u2{0, 0};
+      for (int i = tid; i < heads * (D / 4); i += 64 * W) reinterpret_cast<u2 *>(out)[i] = u2{0, 0};
     return;
   }
   // ---- this wavefront's tiles: t0 + wave, + 4, ...
   const int t0 = span.first + split * p.split_tiles;
   const int nt = span.tiles - split * p.split_tiles < p.split_tiles ? span.tiles - split * p.split_tiles : p.split_tiles;
-  const int mine = (nt - wave + kPagedWaves - 1) / kPagedWaves;  // at least 0
+  const int mine = (nt - wave + W - 1) / W;  // at least 0
   char *kbuf = smem + wave * C::WAVE, *vbuf = kbuf + C::TILE, *sbuf = vbuf + C::TILE;
 
   // -1: not a page, or not a token
   int ids = -1;
   auto take_ids = [&](int j) {
-    const int blk = 2 * (t0 + wave + kPagedWaves * (j + (lane >> 1))) + (lane & 1);
+    const int blk = 2 * (t0 + wave + W * (j + (lane >> 1))) + (lane & 1);
     ids = (int64_t)blk * 16 < span.len && raw >= 0 && raw < p.n_pages ? raw : -1;
   };
   if (p.window != 0) raw = page_of(t0, 0);
@@ -301,7 +304,7 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
   }
 #pragma unroll 1
   for (int j = 0; j < mine; ++j) {
-    const int tile = t0 + wave + kPagedWaves * j;
+    const int tile = t0 + wave + W * j;
     const bool more = j + 1 < mine;
     const bool okA = idA >= 0, okB = idB >= 0;
     // ---- logits
@@ -331,8 +334,8 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
       }
       nextA = __builtin_amdgcn_readlane(ids, 2 * n);
       nextB = __builtin_amdgcn_readlane(ids, 2 * n + 1);
-      ra = row_of(nextA, 2 * (tile + kPagedWaves));
-      rb = row_of(nextB, 2 * (tile + kPagedWaves) + 1);
+      ra = row_of(nextA, 2 * (tile + W));
+      rb = row_of(nextB, 2 * (tile + W) + 1);
       issue(p.k, p.ks, ra, rb, kbuf, sbuf);
     }
     v4f s[2] = {v4f{0, 0, 0, 0}, v4f{0, 0, 0, 0}};
@@ -480,7 +483,7 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
   l = quad_sum(l);
   __syncthreads();
   float *slab = reinterpret_cast<float *>(smem);
-  float *ml = slab + kPagedWaves * kPagedHeads * (D + 4);
+  float *ml = slab + W * kPagedHeads * (D + 4);
   float *mine_at = slab + (wave * kPagedHeads + l16) * (D + 4) + 4 * quad;
 #pragma unroll
   for (int t = 0; t < DT; ++t) {
@@ -493,16 +496,16 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(const
     ml[(wave * kPagedHeads + l16) * 2 + 1] = l;
   }
   __syncthreads();
-  for (int i = tid; i < heads * (D / 4); i += 64 * kPagedWaves) {
+  for (int i = tid; i < heads * (D / 4); i += 64 * W) {
     const int head = i / (D / 4), d4 = i % (D / 4) * 4;
     float top = -INFINITY;
 #pragma unroll
-    for (int s = 0; s < kPagedWaves; ++s) top = fmaxf(top, ml[(s * kPagedHeads + head) * 2]);
+    for (int s = 0; s < W; ++s) top = fmaxf(top, ml[(s * kPagedHeads + head) * 2]);
     const float base = top == -INFINITY ? 0.0f : top;
     v4f o = {0, 0, 0, 0};
     float sum = 0.0f;
 #pragma unroll
-    for (int s = 0; s < kPagedWaves; ++s) {
+    for (int s = 0; s < W; ++s) {
       const float f = __builtin_amdgcn_exp2f(ml[(s * kPagedHeads + head) * 2] - base);
       sum += f * ml[(s * kPagedHeads + head) * 2 + 1];
       o += f * *reinterpret_cast<const v4f *>(slab + (s * kPagedHeads + head) * (D + 4) + d4);
@@ -572,15 +575,22 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedParams p) {
   }
 }
 
-template <int D, bool BF16, bool I8>
-cwac_status launch_paged(const PagedParams &p, hipStream_t st) {
-  constexpr int LDS = PagedCfg<D, I8>::LDS;
+template <int D, bool BF16, bool I8, int W>
+cwac_status launch_parts(const PagedParams &p, hipStream_t st) {
+  constexpr int LDS = PagedCfg<D, I8, W>::LDS;
   static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attention_kernel<D, BF16, I8>),
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attention_kernel<D, BF16, I8, W>),
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (attr != hipSuccess) return CWAC_E_LAUNCH;
-  paged_attention_kernel<D, BF16, I8><<<dim3(p.kv_heads * p.tiles, p.splits, p.batch), 64 * kPagedWaves, LDS, st>>>(p);
-  const cwac_status s = launch_status();
+  paged_attention_kernel<D, BF16, I8, W><<<dim3(p.kv_heads * p.tiles, p.splits, p.batch), 64 * W, LDS, st>>>(p);
+  return launch_status();
+}
+template <int D, bool BF16, bool I8>
+cwac_status launch_paged(const PagedParams &p, hipStream_t st) {
+  if constexpr (D != 256 || I8) {
+    if (p.wide) return launch_parts<D, BF16, I8, kPagedWide>(p, st);
+  }
+  const cwac_status s = launch_parts<D, BF16, I8, kPagedWaves>(p, st);
   if (s != CWAC_OK || p.splits == 1) return s;
   paged_join_kernel<D, BF16><<<dim3(p.q_heads, p.batch), 256, 0, st>>>(p);
   return launch_status();
@@ -630,6 +640,9 @@ extern "C" cwac_status llm_paged_attention(const void *q, int64_t ldq, int32_t t
   PagedParams p{};
   const int64_t tokens = paged_span((int64_t)table_cols * page, window);
   p.splits = paged_splits(batch, q_heads, kv_heads, tokens);
+  // (eight wavefronts' tiles of 16-bit heads of 256 exceed the LDS)
+  p.wide = (head_dim != 256 || int8) && paged_wide(batch, q_heads, kv_heads, head_dim, tokens);
+  if (p.wide) p.splits = 1;
   const int64_t chunk = paged_chunk(tokens, p.splits);
   p.splits = (int)ceil_div(tokens, chunk);
   p.split_tiles = (int)(chunk / kPagedTile);

@@ -8,6 +8,7 @@ namespace cwac {
 
 constexpr int kPagedTile = 32;    // tokens that a wavefront takes at a time
 constexpr int kPagedWaves = 4;    // wavefronts of a workgroup: they take turns over a split's tiles
+constexpr int kPagedWide = 8;     // of one that takes a short length whole
 constexpr int kPagedHeads = 16;   // query heads of one key head that share a workgroup: the columns of the matrix instruction
 constexpr int kPagedMaxSplits = 128;
 
@@ -32,6 +33,19 @@ inline int paged_splits(int64_t batch, int q_heads, int kv_heads, int64_t tokens
   if (tokens / 1024 < even) even = tokens / 1024;
   const int64_t most = fill > even ? fill : even;
   return most < 1 ? 1 : (most > kPagedMaxSplits ? kPagedMaxSplits : (int)most);
+}
+// Whether a length that would be split goes to one workgroup of twice the wavefronts instead, which saves the join: up to two of its turns
+// (one for heads of 256, whose turns take twice as long), or as many as rows fill the chip, a turn for each 20 of them, up to eight.
+// Us without / with: one request of 256 tokens 7.3 / 5.1; 32 rows of 400 7.2 / 6.8, of 700 7.8 / 8.6; 64 rows of 700 10.4 / 9.3,
+// int8 10.0 / 9.9, of 1000 12.1 / 10.6, int8 10.9 / 11.5; 128 rows of 1500 25.5 / 22.0; 256 rows of up to 2000 36.4 / 31.2; 512 rows, int8,
+// of up to 2000 45.9 / 39.6, of up to 3500 64.1 / 63.1; 16 rows of heads of 256, int8, of 256 tokens 9.1 / 7.9, of 400 9.0 / 11.1.
+inline bool paged_wide(int64_t batch, int q_heads, int kv_heads, int head_dim, int64_t tokens) {
+  if (paged_splits(batch, q_heads, kv_heads, tokens) == 1) return false;
+  const int group = q_heads / kv_heads, tiles = (group + kPagedHeads - 1) / kPagedHeads;
+  const int64_t rows = batch * kv_heads * tiles, turn = kPagedTile * kPagedWide, least = head_dim == 256 ? 1 : 2;
+  int64_t turns = rows / 20 > least ? rows / 20 : least;
+  if (turns > 8) turns = 8;
+  return tokens <= turns * turn;
 }
 // Tokens of one split: whole turns.
 inline int64_t paged_chunk(int64_t tokens, int splits) {

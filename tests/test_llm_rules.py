@@ -17,12 +17,14 @@ def rules(tmp_path_factory):
 extern "C" {
 int splits(long long batch, int heads, int kv, long long tokens) { return cwac::paged_splits(batch, heads, kv, tokens); }
 long long chunk(long long tokens, int splits) { return cwac::paged_chunk(tokens, splits); }
+int wide(long long batch, int heads, int kv, int d, long long tokens) { return cwac::paged_wide(batch, heads, kv, d, tokens); }
 long long span(long long cap, int window) { return cwac::paged_span(cap, window); }
 }
 ''')
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I",
                     os.path.join(_ROOT, "paper_2505_20932_amd", "csrc"), str(src), "-o", str(so)], check=True)
     lib, ll, i = C.CDLL(str(so)), C.c_longlong, C.c_int
+    lib.wide.argtypes = [ll, i, i, i, ll]
     lib.splits.argtypes, lib.chunk.argtypes, lib.span.argtypes = [ll, i, i, ll], [ll, i], [ll, i]
     lib.chunk.restype = lib.span.restype = ll
     return lib
@@ -51,3 +53,12 @@ def test_splits_cover_the_tokens_and_fit_the_workspace(rules):
                     c = rules.chunk(n, s)
                     used = -(-n // c)
                     assert c % TURN == 0 and used * c >= n and 1 <= used <= s <= most
+
+
+def test_short_lengths_go_to_one_workgroup(rules):
+    # what was measured on both sides of the rule: rows (requests x key heads), head width, tokens
+    for batch, kv, d, tokens, want in [(1, 32, 128, 256, 1), (1, 32, 128, 400, 1), (1, 32, 128, 700, 0), (1, 8, 128, 1000, 0), (8, 8, 128, 700, 1),
+                                       (8, 8, 128, 1000, 0), (16, 8, 128, 1500, 1), (32, 8, 128, 2000, 1), (32, 8, 128, 3500, 0),
+                                       (64, 8, 128, 2000, 1), (2, 8, 256, 256, 1), (2, 8, 256, 400, 0), (16, 8, 256, 1500, 1),
+                                       (1, 1, 64, 128, 0), (4096, 8, 128, 512, 0)]:
+        assert rules.wide(batch, 4 * kv, kv, d, tokens) == want, (batch, kv, d, tokens)
