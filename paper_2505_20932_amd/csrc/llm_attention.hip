@@ -3,8 +3,8 @@
 //
 // Bound: HBM - every visible key and value is read once, 2 to 32 operations per byte (heads that share a key head share
 // the read); 61 requests of up to 8190 tokens, 8 key heads of 128, bf16: 185 us = 5.5 TB/s, int8 with 5 of up to 131072: 165 us, 5.2 TB/s.  So the kernel is a stream:
-//   * a workgroup takes one request, one key head (up to 16 query heads) and a part of the length; its four wavefronts (eight where
-//     they take a short length whole) take turns over tiles of 32 tokens, each on its own: running maximum, sum and output per
+//   * a workgroup takes one request, one key head (up to 16 query heads) and a part of the length; its four wavefronts (one,
+//     two or eight where they take a short length whole) take turns over tiles of 32 tokens, each on its own: running maximum, sum and output per
 //     wavefront, joined through LDS at the end and, where the length is split, by a second small kernel through the workspace (fixed
 //     order, no atomics);
 //   * keys and values go global -> LDS directly (no registers held while they travel), per 16 tokens one contiguous piece of a page; the
@@ -55,7 +55,7 @@ struct PagedParams {
   int negate;        // scale < 0: the queries change sign
   int batch, q_heads, kv_heads, group, tiles, shift, cols, n_pages, window;
   int splits, split_tiles;
-  int wide;          // kPagedWide wavefronts and no split
+  int log_waves;     // of a workgroup: 1 << log_waves wavefronts
 };
 
 // The part of a request's length that is seen, in tiles, and how many splits it takes.
@@ -72,8 +72,7 @@ struct Span {
   }
 };
 
-// W wavefronts to a workgroup
-template <int D, bool I8, int W>
+template <int D, bool I8>
 struct PagedCfg {
   static constexpr int RB = D * (I8 ? 1 : 2);      // bytes of a row
   static constexpr int CPR = RB / 16;              // 16-byte chunks of it
@@ -83,8 +82,9 @@ struct PagedCfg {
   static constexpr int WAVE = 2 * TILE + 2 * SCALES;  // a wavefront's keys, values and their scales
   static constexpr int LOADS = 2 * LB + (I8 ? 1 : 0);
   static constexpr int SLAB = (D + 4) * 4;            // a head's partial output, 16 bytes apart from the next bank round
-  static constexpr int JOIN = W * (kPagedHeads * SLAB + kPagedHeads * 8);
-  static constexpr int LDS = W * WAVE > JOIN ? W * WAVE : JOIN;
+  static constexpr int JOIN = kPagedHeads * SLAB + kPagedHeads * 8;  // a wavefront's
+  static constexpr int LDS = WAVE > JOIN ? WAVE : JOIN;              // a wavefront's
+  static constexpr int MOST = LDS * kPagedWide <= 160 * 1024 ? kPagedWide : kPagedWaves;  // wavefronts of a workgroup
   // chunk c of row r lies at position c ^ swz(r): 16 rows of one chunk, and 4 x 32-byte pieces of 16 rows, hit distinct banks
   static constexpr int PER = RB >= 256 ? 1 : 256 / RB;  // rows of a bank round
   __host__ __device__ static constexpr int swz(int r) { return (r / PER) & (CPR < 16 ? CPR - 1 : 15); }
@@ -189,11 +189,12 @@ __device__ __forceinline__ float wide(uint16_t h) {
 }
 
 // BF16: the type of the queries and the output, and of a 16-bit cache.
-template <int D, bool BF16, bool I8, int W>
-__global__ __launch_bounds__(64 * W) void paged_attention_kernel(const PagedParams p) {
-  using C = PagedCfg<D, I8, W>;
+template <int D, bool BF16, bool I8>
+__global__ __launch_bounds__((64 * PagedCfg<D, I8>::MOST)) void paged_attention_kernel(const PagedParams p) {
+  using C = PagedCfg<D, I8>;
   constexpr int KS = D / 32, DT = D / 16;
   constexpr bool MB = BF16 && !I8;  // the matrix instructions' type
+  const int W = 1 << p.log_waves;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   // key heads vary fastest: their workgroups read neighbouring pieces of the same pages at about the same time (16 requests, 8 key
   // heads of 256, pages of 64: 137 us with the splits fastest, 107 so)
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(64 * W) void paged_attention_kernel(const PagedPara
   // ---- this wavefront's tiles: t0 + wave, + 4, ...
   const int t0 = span.first + split * p.split_tiles;
   const int nt = span.tiles - split * p.split_tiles < p.split_tiles ? span.tiles - split * p.split_tiles : p.split_tiles;
-  const int mine = (nt - wave + W - 1) / W;  // at least 0
+  const int mine = (nt - wave + W - 1) >> p.log_waves;  // at least 0
   char *kbuf = smem + wave * C::WAVE, *vbuf = kbuf + C::TILE, *sbuf = vbuf + C::TILE;
 
   // -1: not a page, or not a token
@@ -498,18 +499,25 @@ __global__ __launch_bounds__(64 * W) void paged_attention_kernel(const PagedPara
   __syncthreads();
   for (int i = tid; i < heads * (D / 4); i += 64 * W) {
     const int head = i / (D / 4), d4 = i % (D / 4) * 4;
-    float top = -INFINITY;
-#pragma unroll
-    for (int s = 0; s < W; ++s) top = fmaxf(top, ml[(s * kPagedHeads + head) * 2]);
-    const float base = top == -INFINITY ? 0.0f : top;
+    // the wavefronts four at a time (or one or two): their reads are in flight together
+    float top = -INFINITY, sum = 0.0f;
     v4f o = {0, 0, 0, 0};
-    float sum = 0.0f;
+    auto over_waves = [&](auto body) {
+      if (W >= 4) {
+        for (int s0 = 0; s0 < W; s0 += 4)
 #pragma unroll
-    for (int s = 0; s < W; ++s) {
+          for (int s = 0; s < 4; ++s) body(s0 + s);
+      } else {
+        for (int s = 0; s < W; ++s) body(s);
+      }
+    };
+    over_waves([&](int s) { top = fmaxf(top, ml[(s * kPagedHeads + head) * 2]); });
+    const float base = top == -INFINITY ? 0.0f : top;
+    over_waves([&](int s) {
       const float f = __builtin_amdgcn_exp2f(ml[(s * kPagedHeads + head) * 2] - base);
       sum += f * ml[(s * kPagedHeads + head) * 2 + 1];
       o += f * *reinterpret_cast<const v4f *>(slab + (s * kPagedHeads + head) * (D + 4) + d4);
-    }
+    });
     if (span.used == 1) {
       if (sum == 0.0f) sum = 1.0f;  // no token with a page: zeros
       const u2 r = {(uint32_t)narrow<BF16>(o[0] / sum) | (uint32_t)narrow<BF16>(o[1] / sum) << 16,
@@ -575,22 +583,15 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedParams p) {
   }
 }
 
-template <int D, bool BF16, bool I8, int W>
-cwac_status launch_parts(const PagedParams &p, hipStream_t st) {
-  constexpr int LDS = PagedCfg<D, I8, W>::LDS;
-  static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attention_kernel<D, BF16, I8, W>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-  if (attr != hipSuccess) return CWAC_E_LAUNCH;
-  paged_attention_kernel<D, BF16, I8, W><<<dim3(p.kv_heads * p.tiles, p.splits, p.batch), 64 * W, LDS, st>>>(p);
-  return launch_status();
-}
 template <int D, bool BF16, bool I8>
 cwac_status launch_paged(const PagedParams &p, hipStream_t st) {
-  if constexpr (D != 256 || I8) {
-    if (p.wide) return launch_parts<D, BF16, I8, kPagedWide>(p, st);
-  }
-  const cwac_status s = launch_parts<D, BF16, I8, kPagedWaves>(p, st);
+  constexpr int LDS = PagedCfg<D, I8>::LDS, MOST = PagedCfg<D, I8>::MOST * LDS;
+  static_assert(MOST <= 160 * 1024, "LDS of a compute unit");
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attention_kernel<D, BF16, I8>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, MOST);
+  if (attr != hipSuccess) return CWAC_E_LAUNCH;
+  paged_attention_kernel<D, BF16, I8><<<dim3(p.kv_heads * p.tiles, p.splits, p.batch), 64u << p.log_waves, LDS << p.log_waves, st>>>(p);
+  const cwac_status s = launch_status();
   if (s != CWAC_OK || p.splits == 1) return s;
   paged_join_kernel<D, BF16><<<dim3(p.q_heads, p.batch), 256, 0, st>>>(p);
   return launch_status();
@@ -641,8 +642,10 @@ extern "C" cwac_status llm_paged_attention(const void *q, int64_t ldq, int32_t t
   const int64_t tokens = paged_span((int64_t)table_cols * page, window);
   p.splits = paged_splits(batch, q_heads, kv_heads, tokens);
   // (eight wavefronts' tiles of 16-bit heads of 256 exceed the LDS)
-  p.wide = (head_dim != 256 || int8) && paged_wide(batch, q_heads, kv_heads, head_dim, tokens);
-  if (p.wide) p.splits = 1;
+  const bool wide = (head_dim != 256 || int8) && paged_wide(batch, q_heads, kv_heads, head_dim, tokens);
+  if (wide) p.splits = 1;
+  const int waves = wide ? kPagedWide : p.splits == 1 ? paged_waves(tokens) : kPagedWaves;
+  while ((1 << p.log_waves) < waves) ++p.log_waves;
   const int64_t chunk = paged_chunk(tokens, p.splits);
   p.splits = (int)ceil_div(tokens, chunk);
   p.split_tiles = (int)(chunk / kPagedTile);

@@ -18,6 +18,7 @@ extern "C" {
 int splits(long long batch, int heads, int kv, long long tokens) { return cwac::paged_splits(batch, heads, kv, tokens); }
 long long chunk(long long tokens, int splits) { return cwac::paged_chunk(tokens, splits); }
 int wide(long long batch, int heads, int kv, int d, long long tokens) { return cwac::paged_wide(batch, heads, kv, d, tokens); }
+int waves(long long tokens) { return cwac::paged_waves(tokens); }
 long long span(long long cap, int window) { return cwac::paged_span(cap, window); }
 }
 ''')
@@ -62,3 +63,8 @@ def test_short_lengths_go_to_one_workgroup(rules):
                                        (64, 8, 128, 2000, 1), (2, 8, 256, 256, 1), (2, 8, 256, 400, 0), (16, 8, 256, 1500, 1),
                                        (1, 1, 64, 128, 0), (4096, 8, 128, 512, 0)]:
         assert rules.wide(batch, 4 * kv, kv, d, tokens) == want, (batch, kv, d, tokens)
+
+
+def test_no_more_wavefronts_than_tiles(rules):
+    rules.waves.argtypes = [C.c_longlong]
+    assert [rules.waves(n) for n in (1, 16, 32, 33, 64, 65, 128, 5000)] == [1, 1, 1, 2, 2, 4, 4, 4]
