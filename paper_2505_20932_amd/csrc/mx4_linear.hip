@@ -48,19 +48,23 @@ __device__ __forceinline__ v4f mfma16(v4i w, v4i x, v4f acc, int ws, int xs) {
 
 template <int OUT>
 struct OutType;
+// (a row of the output starts at any element, which the vector stores of this device take)
 template <>
 struct OutType<CWAC_OUT_FP32> {
   typedef float T;
+  typedef int Any4i __attribute__((ext_vector_type(4), aligned(4)));
   static __device__ __forceinline__ T make(float u) { return u; }
 };
 template <>
 struct OutType<CWAC_OUT_FP16> {
   typedef uint16_t T;
+  typedef int Any4i __attribute__((ext_vector_type(4), aligned(2)));
   static __device__ __forceinline__ T make(float u) { return __builtin_bit_cast(uint16_t, (_Float16)u); }
 };
 template <>
 struct OutType<CWAC_OUT_BF16> {
   typedef uint16_t T;
+  typedef int Any4i __attribute__((ext_vector_type(4), aligned(2)));
   static __device__ __forceinline__ T make(float u) { return __builtin_bit_cast(uint16_t, (__bf16)u); }
 };
 
@@ -331,7 +335,8 @@ __device__ __forceinline__ v16f mfma32(v4i w, v4i x, v16f acc, int ws, int xs) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(w), operand(x), acc, kE2M1, kE2M1, STEP, ws, STEP, xs);
 }
 
-template <typename C, int OUT>
+// STREAM: the output's stores go past the caches
+template <typename C, int OUT, bool STREAM>
 __global__ __launch_bounds__(C::NT) void mx4_tile_kernel(const Mx4Params p) {
   using O = OutType<OUT>;
   constexpr int TA = C::TA, TB = C::TB, BK = C::BK, NSTAGE = C::NSTAGE;
@@ -544,7 +549,6 @@ __global__ __launch_bounds__(C::NT) void mx4_tile_kernel(const Mx4Params p) {
     const bool more = id < total;
     block ^= 1;
     if (more) open(id, block);
-    const bool whole_lines = p.vec_store && ((en0 * ES) & 15) == 0;
 #pragma unroll
     for (int b = 0; b < TB; ++b)
 #pragma unroll
@@ -571,41 +575,41 @@ __global__ __launch_bounds__(C::NT) void mx4_tile_kernel(const Mx4Params p) {
           }
         // (a wavefront's own slab: its LDS operations are in order)
         typename O::T *o = static_cast<typename O::T *>(p.out) + (em0 + wave_m * 32 * TB + 32 * b) * p.ldo + en0 + wave_n * 32 * TA + 32 * a0;
-        if (whole_lines) {
 #pragma unroll
-          for (int i = 0; i < 32 / RPS; ++i) {
-            const int row = i * RPS + lane / LPR;
-            const v4i v = *reinterpret_cast<const v4i *>(slab + row * ROW + (((lane % LPR) ^ (row & (LPR - 1))) << 4));
-            v4i *dst = reinterpret_cast<v4i *>(o + row * p.ldo + (lane % LPR) * (16 / ES));
-            if constexpr (C::BM == 256)  // these outputs are larger than the L2s: 16384 x 11008 x 4096 394 -> 366 us
-              __builtin_nontemporal_store(v, dst);
-            else
-              *dst = v;
-          }
-        } else {  // whole wavefronts over consecutive elements of a row
-          constexpr int EPR = ROW / ES, LANES = EPR < 64 ? EPR : 64;
-          for (int row = lane / LANES; row < 32; row += 64 / LANES)
-#pragma unroll
-            for (int e = lane % LANES; e < EPR; e += LANES)
-              o[row * p.ldo + e] =
-                  *reinterpret_cast<const typename O::T *>(slab + row * ROW + ((((e * ES) >> 4) ^ (row & (LPR - 1))) << 4) + ((e * ES) & 15));
+        for (int i = 0; i < 32 / RPS; ++i) {
+          const int row = i * RPS + lane / LPR;
+          const v4i v = *reinterpret_cast<const v4i *>(slab + row * ROW + (((lane % LPR) ^ (row & (LPR - 1))) << 4));
+          auto *dst = reinterpret_cast<typename O::Any4i *>(o + row * p.ldo + (lane % LPR) * (16 / ES));
+          if constexpr (STREAM)
+            __builtin_nontemporal_store(v, dst);
+          else
+            *dst = v;
         }
       }
     if (!more) break;
-    stored = whole_lines;
+    stored = true;
     wait_lds();
     __builtin_amdgcn_s_barrier();  // every slab is read: the stages under them are free
     __builtin_amdgcn_sched_barrier(0);
   }
 }
 
-template <typename C, int OUT>
+template <typename C, int OUT, bool STREAM>
 cwac_status launch_tile_one(const Mx4Params &p, unsigned blocks, hipStream_t st) {
   static const hipError_t attr =
-      hipFuncSetAttribute(reinterpret_cast<const void *>(&mx4_tile_kernel<C, OUT>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+      hipFuncSetAttribute(reinterpret_cast<const void *>(&mx4_tile_kernel<C, OUT, STREAM>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
   if (attr != hipSuccess) return CWAC_E_LAUNCH;
-  mx4_tile_kernel<C, OUT><<<blocks, C::NT, C::LDS, st>>>(p);
+  mx4_tile_kernel<C, OUT, STREAM><<<blocks, C::NT, C::LDS, st>>>(p);
   return launch_status();
+}
+// The large tiles' outputs are larger than the L2s and go past the caches (16384 x 11008 x 4096 394 -> 348 us), unless rows begin inside
+// a line: the line that two stores share would cross to memory twice (7567 x 9129 x 896 bf16 87 / 102, fp32 128 / 163).
+template <typename C, int OUT>
+cwac_status launch_tile_out(const Mx4Params &p, unsigned blocks, hipStream_t st) {
+  if constexpr (C::BM == 256) {
+    if (aligned(p.out, 64) && p.ldo * (int64_t)sizeof(typename OutType<OUT>::T) % 64 == 0) return launch_tile_one<C, OUT, true>(p, blocks, st);
+  }
+  return launch_tile_one<C, OUT, false>(p, blocks, st);
 }
 
 template <typename C>
@@ -617,9 +621,9 @@ cwac_status launch_tile(Mx4Params p, int out_kind, hipStream_t st) {
   // as many persistent workgroups as fit the chip (256 compute units); a multiple of 8 keeps a workgroup's tiles on one XCD
   const int64_t fit = 256 * (160 * 1024 / C::LDS);
   const unsigned blocks = (unsigned)(tiles < fit ? tiles : fit);
-  if (out_kind == CWAC_OUT_FP32) return launch_tile_one<C, CWAC_OUT_FP32>(p, blocks, st);
-  if (out_kind == CWAC_OUT_FP16) return launch_tile_one<C, CWAC_OUT_FP16>(p, blocks, st);
-  return launch_tile_one<C, CWAC_OUT_BF16>(p, blocks, st);
+  if (out_kind == CWAC_OUT_FP32) return launch_tile_out<C, CWAC_OUT_FP32>(p, blocks, st);
+  if (out_kind == CWAC_OUT_FP16) return launch_tile_out<C, CWAC_OUT_FP16>(p, blocks, st);
+  return launch_tile_out<C, CWAC_OUT_BF16>(p, blocks, st);
 }
 
 using Tile256 = Mx4TileCfg<256, 256, 4, 4, 2>;      // eight wavefronts of 64 x 128, one workgroup per compute unit
