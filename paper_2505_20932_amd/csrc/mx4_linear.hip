@@ -296,7 +296,7 @@ cwac_status launch_split(Mx4Params p, int out_kind, hipStream_t st) {
 // ------------------------------------------------------------------------------------------
 // Many tiles: BM tokens x BN channels at a time, both panels through a ring of NSTAGE stages in LDS, one stage = one panel of 256
 // values (128 bytes of codes and 8 scale bytes per row).  Bound: the matrix cores, under the device's power limit: 16384 x 4096 x 11008 bf16
-// 335-340 us = 4.4 PFLOP/s (4.8 over K alone), where the instruction by itself sustains 5.2 on random codes; they are busy for 62 % of
+// 333 us = 4.4 PFLOP/s (4.8 over K alone), where the instruction by itself sustains 5.2 on random codes; they are busy for 62 % of
 // the cycles at 1.63 GHz.  128 x 128 tiles read as many LDS cycles as they multiply and take 0.4 us a stage.
 //   * Codes go global -> LDS directly, 8 rows x 128 bytes per load; the 16-byte chunk c of row r lands at position c ^ ((r >> 1) & 7)
 //     (applied on the global side), so operand reads are free of bank conflicts.  Buffer loads whose descriptor moves along K with

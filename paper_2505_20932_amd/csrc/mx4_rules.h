@@ -11,19 +11,22 @@ namespace cwac {
 // Split-K kernel, channels x tokens; tiles of 128 x 128, one workgroup per compute unit with three stages or two with two; 256 x 256.
 enum { kMx4Split16 = 1, kMx4Split32x16, kMx4Split32, kMx4Split64, kMx4Tile128Deep, kMx4Tile128Pair, kMx4Tile256 };
 
-// Estimated microseconds, fitted to 200 layers of 96 to 8192 tokens (weights cold, P = panels of 256 values of K).  A round is what the
+// Estimated microseconds, fitted to 147 layers of 96 to 8192 tokens (weights cold, P = panels of 256 values of K), the two last to 110
+// layers of 400 to 16384 tokens and any width (off by 9 and 6 % in the mean; the choice costs 1 % over the best).  A round is what the
 // chip holds at once: 512 tiles of 32 x 32 (256 of 64 x 64), 256 or 512 of 128 x 128, 256 of 256 x 256.
 //   tokens x channels x K          split 32   split 64   128 deep   128 pair   256      (measured)
-//   128 x 4096 x 4096                 6.1        8.6       10.7       14.5       -
-//   256 x 4096 x 4096                 9.9        8.7       10.9       14.6      25.0
-//   601 x 4096 x 4096                19.9       22.2       11.8       15.3      25.2
-//   256 x 4096 x 11008               23.6       17.7       29.5       41.0      69.7
-//   601 x 2304 x 768                  7.6        9.2        6.6        6.8      12.1
-//   2048 x 4096 x 4096               67         62         28.8       25.4      35.5
-//   4096 x 4096 x 4096              125        122         54.7       47.2      43.4
-//   1500 x 11008 x 4096             120        119         57.9       55.7      63.5   (258 tiles of 256 x 256)
-//   4096 x 11008 x 4096             324        327        150        134       111
-//   8192 x 2304 x 768                70         72         28.7       22.7      28.4
+//   128 x 4096 x 4096                 6.1        8.6       11.2       14.5       -
+//   256 x 4096 x 4096                 9.9        8.7       11.4       14.6      23.8
+//   601 x 4096 x 4096                19.9       22.2       12.4       15.2      23.9
+//   256 x 4096 x 11008               23.6       17.7       30.7       41.5      68.3
+//   601 x 2304 x 768                  7.6        9.2        6.7        7.0      10.6
+//   2048 x 4096 x 4096               67         62         29.0       25.5      26.7
+//   4096 x 4096 x 4096              125        122         55.9       47.9      37.4
+//   1500 x 11008 x 4096             120        119         57.5       55.4      54.8   (258 tiles of 256 x 256)
+//   2721 x 4586 x 8288                -          -         96.2       91.4      61.3
+//   12757 x 4565 x 1024               -          -         78.1       59.0      70.6
+//   4096 x 11008 x 4096             324        327        148        131        94.3
+//   8192 x 2304 x 768                70         72         29.5       23.2      23.2
 inline double mx4_split32_us(int64_t m, int n, int k) {
   const double p = (double)((k + 255) / 256), x = (double)tiles_of(m, n, 32, 32) / 512.0;
   return 1.8 + (x < 1.0 ? (x < 0.5 ? 0.6 : 0.2 + 0.8 * x) : x) * (1.2 + 0.225 * p);
@@ -38,14 +41,14 @@ inline double mx4_tile128_deep_us(int64_t m, int n, int k) {  // one round; more
   return tiles_of(m, n, 128, 128) <= 256 ? 5.2 + 0.3 * p + 0.006 * p * p : 1e30;
 }
 inline double mx4_tile128_pair_us(int64_t m, int n, int k) {
-  const double p = (double)((k + 255) / 256), x = (double)tiles_of(m, n, 128, 128) / 512.0;
-  if (x <= 0.5) return 5.0 + 0.7 * p;
-  return (x + 0.07 < 0.95 ? 0.95 : x + 0.07) * (6.4 + 1.05 * p);
+  const double p = (double)((k + 255) / 256);
+  const int64_t t = tiles_of(m, n, 128, 128), full = t / 512, rest = t % 512;
+  return 5.8 + ((double)full + (rest ? 0.43 + 0.51 * (double)rest / 512.0 : 0.0)) * (3.2 + 1.14 * p + 0.0038 * p * p);
 }
 inline double mx4_tile256_us(int64_t m, int n, int k) {
   const double p = (double)((k + 255) / 256);
   const int64_t t = tiles_of(m, n, 256, 256), full = t / 256, rest = t % 256;
-  return ((double)full * 1.1 + (rest ? 0.62 + 0.5 * (double)rest / 256.0 : 0.0)) * (9.0 + 1.75 * p);
+  return 1.1 + ((double)full + (rest ? 0.68 + 0.31 * (double)rest / 256.0 : 0.0)) * (11.4 + 1.59 * p + 0.00125 * p * p);
 }
 
 inline int mx4_split_form(int64_t m, int n, int k) {
