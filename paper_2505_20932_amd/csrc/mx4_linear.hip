@@ -33,7 +33,6 @@ struct Mx4Params {
   int n, k;
   const float *mult, *fbias;
   void *out;
-  int vec_store;  // output rows and base are 16-byte aligned
   int tiles_m, tiles_n;
 };
 
@@ -53,18 +52,21 @@ template <>
 struct OutType<CWAC_OUT_FP32> {
   typedef float T;
   typedef int Any4i __attribute__((ext_vector_type(4), aligned(4)));
+  typedef float Any4 __attribute__((ext_vector_type(4), aligned(4)));
   static __device__ __forceinline__ T make(float u) { return u; }
 };
 template <>
 struct OutType<CWAC_OUT_FP16> {
   typedef uint16_t T;
   typedef int Any4i __attribute__((ext_vector_type(4), aligned(2)));
+  typedef uint16_t Any4 __attribute__((ext_vector_type(4), aligned(2)));
   static __device__ __forceinline__ T make(float u) { return __builtin_bit_cast(uint16_t, (_Float16)u); }
 };
 template <>
 struct OutType<CWAC_OUT_BF16> {
   typedef uint16_t T;
   typedef int Any4i __attribute__((ext_vector_type(4), aligned(2)));
+  typedef uint16_t Any4 __attribute__((ext_vector_type(4), aligned(2)));
   static __device__ __forceinline__ T make(float u) { return __builtin_bit_cast(uint16_t, (__bf16)u); }
 };
 
@@ -259,11 +261,8 @@ __global__ __launch_bounds__(64 * W) void mx4_splitk_kernel(const Mx4Params p) {
       u[r] = O::make(f);
     }
     typename O::T *o = static_cast<typename O::T *>(p.out) + (bm0 + row) * p.ldo + nn;
-    if (p.vec_store && nn + 3 < p.n) {
-      if constexpr (sizeof(typename O::T) == 4)
-        *reinterpret_cast<v4f *>(o) = v4f{u[0], u[1], u[2], u[3]};
-      else
-        *reinterpret_cast<uint2 *>(o) = make_uint2((uint32_t)u[0] | (uint32_t)u[1] << 16, (uint32_t)u[2] | (uint32_t)u[3] << 16);
+    if (nn + 3 < p.n) {
+      *reinterpret_cast<typename O::Any4 *>(o) = typename O::Any4{u[0], u[1], u[2], u[3]};
     } else {
 #pragma unroll
       for (int r = 0; r < 4; ++r)
@@ -653,7 +652,6 @@ extern "C" cwac_status qlinear_mx4_cwac_forward_ex(const uint8_t *x_codes, int64
   p.x = x_codes, p.w = w_codes, p.xs = x_scales, p.ws = w_scales;
   p.ldx = ldx, p.ldw = ldw, p.ldo = ldo, p.m = m, p.n = n, p.k = k;
   p.mult = mult, p.fbias = fbias, p.out = out;
-  p.vec_store = aligned(out, 16) && (ldo * size) % 16 == 0;
   hipStream_t st = as_stream(stream);
   int form = mx4_form(m, n, k);
   if (tune.kernel == CWAC_KERNEL_SPLIT_K) form = mx4_split_form(m, n, k);
