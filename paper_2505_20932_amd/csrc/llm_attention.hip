@@ -15,12 +15,13 @@
 //     that order - the weights never change lanes.  The values come out of LDS transposed (the transposing reads of this device).
 //     One query head uses one of 16 columns; the matrix cores are idle otherwise;
 //   * an 8-bit cache is widened to binary16 in registers (exact); the keys' scales multiply the logits, the values' scales the
-//     weights, relative to a running power of two so that small ones lose nothing.  bfloat16 queries become binary16 relative to
+//     weights, relative to a running power of two above every scale so far.  bfloat16 queries become binary16 relative to
 //     the head's largest one (what falls below 2^-25 of that is lost).
-// Weights meet the values as a sum of two numbers of the matrix instruction's type (off by 2^-20 of a weight at most in binary16, the two
-// cut off rather than rounded, which is one instruction for a pair; 2^-17 in bfloat16).  One binary16 number would be off by 2^-11 and lets
-// int8 caches' outputs be 1.7 times as far from the exact ones; the second one's matrix instructions wait for nothing (five requests
-// of 30011 to 131072 tokens 173.8 us either way).  Maximum, sum and output are fp32.
+// Weights meet the values as a sum of two numbers of the matrix instruction's type (off by 2^-17 of a weight in bfloat16; by 2^-20 in
+// binary16, whose two are cut off rather than rounded, which is one instruction for a pair).  binary16 has no steps below 2^-24, so the weights take
+// its whole range: the largest one is 2^15, and what lies below 2^-19 of it is off by up to 2^-39 of it.  One binary16 number would be off by
+// 2^-11 and lets int8 caches' outputs be 1.7 times as far from the exact ones; the second one's matrix instructions wait for nothing
+// (five requests of 30011 to 131072 tokens 173.8 us either way).  Maximum, sum and output are fp32.
 // Tokens outside [lo, len), and those of a page whose number is not one, get weight 0, and what the cache holds there is
 // replaced by 0, NaN included.
 #include <type_traits>
@@ -293,7 +294,8 @@ __global__ __launch_bounds__((64 * PagedCfg<D, I8>::MOST)) void paged_attention_
 #pragma unroll
   for (int i = 0; i < DT; ++i) acc[i] = v4f{0, 0, 0, 0};
   float m = -INFINITY, l = 0.0f;  // maximum of the logits before the factor c, sum of the weights of this lane's tokens
-  float unit = 0x1p-126f, per_unit = 0x1p126f;  // of acc (8-bit caches): a power of two above every value scale so far
+  // binary16 weights are multiplied by 2^15 / unit and so is acc; unit: a power of two above every value scale so far (8-bit caches)
+  float unit = I8 ? 0x1p-111f : 1.0f, per_unit = I8 ? 0x1p126f : 0x1p15f;
 
   int idA = -1, idB = -1;
   if (mine > 0) {
@@ -444,13 +446,16 @@ __global__ __launch_bounds__((64 * PagedCfg<D, I8>::MOST)) void paged_attention_
       for (int i = 0; i < 8; ++i) big = fmaxf(big, vsc[i >> 2][i & 3]);
       if (__builtin_amdgcn_ballot_w64(big > unit)) {  // rare: a larger scale than any before
         const int e = __builtin_amdgcn_frexp_expf(fmaxf(quad_max(big), unit));
-        const float next = e < 126 ? __builtin_amdgcn_ldexpf(1.0f, e) : 0x1p126f;
+        const float next = e < 127 ? __builtin_amdgcn_ldexpf(1.0f, e) : 0x1p127f;
         alpha *= unit / next;
         unit = next;
-        per_unit = 1.0f / next;
+        per_unit = 0x1p15f / next;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] *= vsc[i >> 2][i & 3] * per_unit;
+    } else if (!MB) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] *= 0x1p15f;
     }
     u4 hi, lo;
 #pragma unroll
@@ -489,7 +494,7 @@ __global__ __launch_bounds__((64 * PagedCfg<D, I8>::MOST)) void paged_attention_
 #pragma unroll
   for (int t = 0; t < DT; ++t) {
     v4f o = acc[t];
-    if (I8) o *= unit;
+    if (!MB) o *= unit * 0x1p-15f;
     *reinterpret_cast<v4f *>(mine_at + 16 * t) = o;
   }
   if (quad == 0) {
