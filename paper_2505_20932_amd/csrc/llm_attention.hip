@@ -15,11 +15,13 @@
 //     that order - the weights never change lanes.  The values come out of LDS transposed (the transposing reads of this device).
 //     One query head uses one of 16 columns; the matrix cores are idle otherwise;
 //   * an 8-bit cache is widened to binary16 in registers (exact); the keys' scales multiply the logits, the values' scales the
-//     weights, relative to a running power of two above every scale so far.  bfloat16 queries become binary16 relative to
+//     weights, relative to a power of two that follows a head's largest product of the two.  bfloat16 queries become binary16 relative to
 //     the head's largest one (what falls below 2^-25 of that is lost).
 // Weights meet the values as a sum of two numbers of the matrix instruction's type (off by 2^-17 of a weight in bfloat16; by 2^-20 in
 // binary16, whose two are cut off rather than rounded, which is one instruction for a pair).  binary16 has no steps below 2^-24, so the weights take
-// its whole range: the largest one is 2^15, and what lies below 2^-19 of it is off by up to 2^-39 of it.  One binary16 number would be off by
+// its whole range: the largest one (8 bits: weight times scale) is 2^15 (8 bits: 2^10 to 2^15), and what lies far below it is off by up to 2^-39 (2^-34) of
+// it.  A power of two above every scale so far would let one token of large values and no weight spoil all others: 0.5 % at
+// 2^16 times their scale, 8 % at 2^20.  One binary16 number would be off by
 // 2^-11 and lets int8 caches' outputs be 1.7 times as far from the exact ones; the second one's matrix instructions wait for nothing
 // (five requests of 30011 to 131072 tokens 173.8 us either way).  Maximum, sum and output are fp32.
 // Tokens outside [lo, len), and those of a page whose number is not one, get weight 0, and what the cache holds there is
@@ -294,8 +296,9 @@ __global__ __launch_bounds__((64 * PagedCfg<D, I8>::MOST)) void paged_attention_
 #pragma unroll
   for (int i = 0; i < DT; ++i) acc[i] = v4f{0, 0, 0, 0};
   float m = -INFINITY, l = 0.0f;  // maximum of the logits before the factor c, sum of the weights of this lane's tokens
-  // binary16 weights are multiplied by 2^15 / unit and so is acc; unit: a power of two above every value scale so far (8-bit caches)
-  float unit = I8 ? 0x1p-111f : 1.0f, per_unit = I8 ? 0x1p126f : 0x1p15f;
+  // Binary16 weights, and so acc, are multiplied by a power of two.  8-bit caches: times the value's scale first, whose largest product so far,
+  // as much of it as the maximum of the logits leaves, is `peak` in one of a head's four lanes
+  float per = I8 ? 0x1p126f : 0x1p15f, peak = 0.0f;
 
   int idA = -1, idB = -1;
   if (mine > 0) {
@@ -443,16 +446,30 @@ __global__ __launch_bounds__((64 * PagedCfg<D, I8>::MOST)) void paged_attention_
     if (I8) {
       float big = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) big = fmaxf(big, vsc[i >> 2][i & 3]);
-      if (__builtin_amdgcn_ballot_w64(big > unit)) {  // rare: a larger scale than any before
-        const int e = __builtin_amdgcn_frexp_expf(fmaxf(quad_max(big), unit));
-        const float next = e < 127 ? __builtin_amdgcn_ldexpf(1.0f, e) : 0x1p127f;
-        alpha *= unit / next;
-        unit = next;
-        per_unit = 0x1p15f / next;
+      for (int i = 0; i < 8; ++i) {
+        w[i] *= vsc[i >> 2][i & 3];
+        big = fmaxf(big, fabsf(w[i]));
+      }
+      peak = fmaxf(peak * alpha, big);
+      const float at = peak * per;
+      const uint64_t over = __builtin_amdgcn_ballot_w64(at > 0x1p15f);
+      if (over | __builtin_amdgcn_ballot_w64(alpha != 1.0f)) {  // after the first tiles neither is frequent
+        // the heads of which some lane has at least 2^10 (only a new maximum can have lowered it), or that cannot be raised
+        const uint64_t lanes = __builtin_amdgcn_ballot_w64(at >= 0x1p10f || per >= 0x1p126f);
+        uint32_t fit = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+        fit |= fit >> 16;
+        if (over || (fit & 0xffff) != 0xffff) {
+          peak = quad_max(peak);
+          const float next = __builtin_amdgcn_ldexpf(1.0f, 15 - __builtin_amdgcn_frexp_expf(fmaxf(peak, 0x1p-112f)));
+          // (at most 2^6: acc was in proportion to the peak that alpha has lowered)
+          alpha = __builtin_amdgcn_ldexpf(alpha, __builtin_amdgcn_frexp_expf(next) - __builtin_amdgcn_frexp_expf(per));
+          per = next;
+        }
+#pragma unroll
+        for (int t = 0; t < DT; ++t) acc[t] *= alpha;
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] *= vsc[i >> 2][i & 3] * per_unit;
+      for (int i = 0; i < 8; ++i) w[i] *= per;
     } else if (!MB) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] *= 0x1p15f;
@@ -470,7 +487,7 @@ __global__ __launch_bounds__((64 * PagedCfg<D, I8>::MOST)) void paged_attention_
         lo[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(w[2 * i] - (float)a[0], w[2 * i + 1] - (float)a[1]));
       }
     }
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {  // after the first tiles a maximum seldom moves
+    if (!I8 && __builtin_amdgcn_ballot_w64(alpha != 1.0f)) {  // after the first tiles a maximum seldom moves
 #pragma unroll
       for (int t = 0; t < DT; ++t) acc[t] *= alpha;
     }
@@ -494,7 +511,7 @@ __global__ __launch_bounds__((64 * PagedCfg<D, I8>::MOST)) void paged_attention_
 #pragma unroll
   for (int t = 0; t < DT; ++t) {
     v4f o = acc[t];
-    if (!MB) o *= unit * 0x1p-15f;
+    if (!MB) o *= 1.0f / per;
     *reinterpret_cast<v4f *>(mine_at + 16 * t) = o;
   }
   if (quad == 0) {

@@ -46,7 +46,8 @@ def _cache(n, cols, heads, kv, d, t, cache, special, seed):
 
 
 def _reference(q, kc, vc, ks, vs, n):
-    """Per head: the output, sum w |v|, the largest sum of |q k|, the largest |v| (8-bit cache: value scale)."""
+    """Per head: the output, sum w |v|, the largest sum of |q k|, the largest |v| (8-bit cache: the largest w * s over the
+    values' scales s)."""
     def rows(c, s):
         x = c.double() if s is None else c.double() * s.double()[..., None]
         return x.transpose(1, 2).reshape(-1, c.shape[1], c.shape[3])[:n].cpu().numpy()
@@ -62,7 +63,7 @@ def _reference(q, kc, vc, ks, vs, n):
         out[h], mag[h] = w @ v[:, g], w @ np.abs(v[:, g])
         qk[h] = SCALE * (np.abs(k[:, g]) @ np.abs(qn[h])).max()
         unit = np.abs(v[:, g]).max(axis=1) if vs is None else vs.double().transpose(1, 2).reshape(-1, kc.shape[1])[:n, g].cpu().numpy()
-        peak[h] = unit.max()
+        peak[h] = unit.max() if vs is None else (w * unit).max()
     return out, mag, qk, peak
 
 
@@ -83,8 +84,8 @@ def _run(n, cols, heads, kv, d, t, cache, special, seed=0):
         logit = logit + d * 2.0 ** -24 * float(q.abs().max()) * top * SCALE
     rel = (2.0 ** -20 if half else 2.0 ** -16) + 2 * logit + 2.0 ** -23 * (n + 16)
     # Absolute, per token: binary16's smallest step, 2^-24.  16 bit: the largest weight is 2^15 (and their sum no less), so 2^-39 of the largest value.
-    # 8 bit: a weight times its scale is 2^15 next to a power of two of at most twice the largest scale, a code at most 127.
-    step = 0.0 if not half else n * (2.0 ** -39 * peak if cache != "i8" else 2.0 ** -38 * 127 * peak)
+    # 8 bit: where a weight times its scale is largest it is 2^10 or more, so 2^-34 of it next to codes of at most 127.
+    step = 0.0 if not half else n * (2.0 ** -39 * peak if cache != "i8" else 2.0 ** -34 * 127 * peak)
     tol = EPS[t] * np.abs(want) + (rel[:, None] * mag + np.reshape(step, (-1, 1))) * 1.01 + (2.0 ** -25 if t == "f16" else 2.0 ** -134)
     got = out[0].double().cpu().numpy()
     assert np.isfinite(got).all()
@@ -101,3 +102,28 @@ def test_a_token_of_nearly_all_the_weight_and_no_values(shape, t, cache, gap):
     """The output is what the others' small weights bring."""
     for at in (0, shape[0] - 1):
         _run(*shape, t, cache, {at: (float(gap), 0.0)})
+
+
+UNEVEN = [("bf16", "bf16"), ("f16", "i8"), ("bf16", "i8")]
+
+
+@pytest.mark.parametrize("factor", [6, 10, 13, 16, 20, 40])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("t,cache", UNEVEN)
+def test_a_token_of_large_values_and_no_weight(shape, t, cache, factor):
+    """Values 2^factor times the others' at e^-50 of their weight: the others' output."""
+    for at in (0, shape[0] // 2, shape[0] - 1):
+        _run(*shape, t, cache, {at: (-50.0, 2.0 ** factor)})
+
+
+@pytest.mark.parametrize("factor", [-20, 4, 16, 24])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("t,cache", UNEVEN)
+def test_large_values_lose_their_weight(shape, t, cache, factor):
+    """Tokens of other values lead for a while; then come logits that leave them e^-40.  And the other way round."""
+    n = shape[0]
+    early, late = range(0, max(1, n // 4)), range(n - max(1, n // 4), n)
+    for low, high in ((early, late), (late, early)):
+        special = {i: (3.0 + 0.01 * (i % 7), 2.0 ** factor) for i in low}
+        special.update({i: (43.0 + 0.1 * (i % 11), 1.0) for i in high})
+        _run(*shape, t, cache, special)
