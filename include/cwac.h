@@ -517,7 +517,8 @@ enum { CWAC_KV_MAX_BATCH = 8192 };
  *   need = ceil((old + new) / page) - ceil(old / page) pages are taken from the top of the stack free_pages[0 .. n_free), for
  *   the requests in order: the first page is free_pages[n_free - 1].  A request whose table row is too short for it takes none
  *   and is not served; one whose pages are beyond the end of the stack (those of the requests before it
- *   included) is not served either.
+ *   included) is not served either, nor is one whose rows do not all lie in [0, slot_capacity): its tokens could not be appended.  With
+ *   slot_capacity 0 no slots are asked for, and pages are given all the same (a reservation).
  *   table        in/out: the new pages' entries are written, others left
  *   slots        device int64 [slot_capacity]: the slot of every new token in batch order; -1 for tokens of requests not
  *                served, for tokens of a page whose entry is negative, and for rows behind the last token

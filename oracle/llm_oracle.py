@@ -5,7 +5,8 @@ TINY = np.float32(2.0 ** -118)                      # FLT_MIN * 256: the smalles
 
 
 def assign_pages(old, new, page, free, n_free, table, slot_capacity):
-    """-> (table, slots, token_start, seq_lens, n_left): requests in order, pages from the top of the free stack."""
+    """-> (table, slots, token_start, seq_lens, n_left): requests in order, pages from the top of the free stack; one
+    whose rows do not all have a slot is not served (slot_capacity 0: no slots are asked for)."""
     table = np.array(table, dtype=np.int32)
     slots = np.full(slot_capacity, -1, dtype=np.int64)
     n_free = min(max(int(n_free), 0), len(free))
@@ -15,7 +16,8 @@ def assign_pages(old, new, page, free, n_free, table, slot_capacity):
         have, end = -(-o // page), -(-(o + w) // page)
         fits = end <= table.shape[1]
         need = end - have if fits else 0
-        served = fits and (need == 0 or asked + need <= n_free)
+        rows = w == 0 or slot_capacity == 0 or row + w <= min(slot_capacity, 2 ** 31 - 1)
+        served = fits and rows and (need == 0 or asked + need <= n_free)
         start.append(min(row, 2 ** 31 - 1))
         if served:
             for i in range(need):

@@ -84,7 +84,9 @@ __global__ __launch_bounds__(kThreads) void kv_assign_kernel(const AssignParams 
     const int b = first + i;
     const Request r(p, b);
     const uint32_t g1 = sat(g0, r.need);
-    const bool served = r.fits && (r.need == 0 || (uint64_t)g0 + r.need <= (uint32_t)n_free);
+    // rows without a slot cannot be appended: such a request takes no pages (nor do those behind it, whose rows lie further back)
+    const bool rows = r.new_len == 0 || p.capacity == 0 || (uint64_t)t0 + r.new_len <= (uint64_t)(p.capacity < kTop ? p.capacity : kTop);
+    const bool served = r.fits && rows && (r.need == 0 || (uint64_t)g0 + r.need <= (uint32_t)n_free);
     page_at[b] = served ? g0 : kNot;
     old_at[b] = r.old_len;
     if (served && r.need) taken = g1;
