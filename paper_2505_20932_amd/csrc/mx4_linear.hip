@@ -34,6 +34,7 @@ struct Mx4Params {
   const float *mult, *fbias;
   void *out;
   int tiles_m, tiles_n;
+  int first;  // tile of the launch's first workgroup (split-K forms)
 };
 
 // The operand of an instruction: 32 codes, the lower half of the register block that other formats fill.
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(64 * W) void mx4_splitk_kernel(const Mx4Params p) {
   using O = OutType<OUT>;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   int tile_m, tile_n;
-  tile_of_block(blockIdx.x, p.tiles_m, p.tiles_n, tile_m, tile_n);
+  tile_of_block(p.first + (int)blockIdx.x, p.tiles_m, p.tiles_n, tile_m, tile_n);
   const int64_t bm0 = (int64_t)tile_m * C::BM;
   const int bn0 = tile_n * C::BN;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -272,24 +273,31 @@ __global__ __launch_bounds__(64 * W) void mx4_splitk_kernel(const Mx4Params p) {
 }
 
 template <int TN, int TM, int W, int D, int OUT>
-cwac_status launch_split_one(const Mx4Params &p, unsigned blocks, hipStream_t st) {
+cwac_status launch_split_one(Mx4Params p, int64_t tiles, hipStream_t st) {
   constexpr int LDS = Mx4SplitCfg<TN, TM, W, D>::LDS_BYTES;
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(&mx4_splitk_kernel<TN, TM, W, D, OUT>),
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (attr != hipSuccess) return CWAC_E_LAUNCH;
-  mx4_splitk_kernel<TN, TM, W, D, OUT><<<blocks, 64 * W, LDS, st>>>(p);
-  return launch_status();
+  static_assert(64 * W <= 256, "kMx4TilesPerLaunch");
+  for (int64_t at = 0; at < tiles; at += kMx4TilesPerLaunch) {
+    p.first = (int)at;
+    const int64_t blocks = tiles - at < kMx4TilesPerLaunch ? tiles - at : kMx4TilesPerLaunch;
+    mx4_splitk_kernel<TN, TM, W, D, OUT><<<(unsigned)blocks, 64 * W, LDS, st>>>(p);
+    const cwac_status s = launch_status();
+    if (s != CWAC_OK) return s;
+  }
+  return CWAC_OK;
 }
 
 template <int TN, int TM, int W, int D>
 cwac_status launch_split(Mx4Params p, int out_kind, hipStream_t st) {
   p.tiles_m = (int)ceil_div(p.m, 16 * TM);
   p.tiles_n = (int)ceil_div(p.n, 16 * TN);
-  const int64_t blocks = (int64_t)p.tiles_m * p.tiles_n;
-  if (blocks > 0x7fffffff) return CWAC_E_SHAPE;
-  if (out_kind == CWAC_OUT_FP32) return launch_split_one<TN, TM, W, D, CWAC_OUT_FP32>(p, (unsigned)blocks, st);
-  if (out_kind == CWAC_OUT_FP16) return launch_split_one<TN, TM, W, D, CWAC_OUT_FP16>(p, (unsigned)blocks, st);
-  return launch_split_one<TN, TM, W, D, CWAC_OUT_BF16>(p, (unsigned)blocks, st);
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+  if (tiles > 0x3fffffff) return CWAC_E_SHAPE;  // (an output of 2^38 elements or more; a tile's number and that of a tile row's eight stay in 32 bits)
+  if (out_kind == CWAC_OUT_FP32) return launch_split_one<TN, TM, W, D, CWAC_OUT_FP32>(p, tiles, st);
+  if (out_kind == CWAC_OUT_FP16) return launch_split_one<TN, TM, W, D, CWAC_OUT_FP16>(p, tiles, st);
+  return launch_split_one<TN, TM, W, D, CWAC_OUT_BF16>(p, tiles, st);
 }
 
 // ------------------------------------------------------------------------------------------

@@ -72,4 +72,7 @@ inline int mx4_form(int64_t m, int n, int k) {
   return form;
 }
 
+// Workgroups of one launch of the split-K forms (256 threads each; a grid counts fewer than 2^32 threads); more tiles take several.
+constexpr int64_t kMx4TilesPerLaunch = ((int64_t)1 << 31) / 256;
+
 }  // namespace cwac
