@@ -1,5 +1,6 @@
 // The paged key-value cache of a language model: pages for a step's new tokens, and the tokens' keys and values into them.
 #include "cwac_internal.h"
+#include "llm_rules.h"
 
 namespace cwac {
 namespace {
@@ -164,6 +165,7 @@ struct AppendParams {
   int heads, log_pieces, shift;  // pieces of 16 bytes of a head: 1 << log_pieces
   uint32_t pieces;               // of a row: heads << log_pieces
   uint32_t units;                // of a step's TOK tokens: 2 * pieces, the keys' first
+  int64_t first;                 // workgroup of the call that the launch begins with
 };
 
 template <bool BF16>
@@ -182,7 +184,7 @@ __device__ __forceinline__ void widen(u4 a, float (&f)[8]) {
 
 template <bool INT8, bool BF16, int TOK>
 __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(const AppendParams p) {
-  const uint64_t id = (uint64_t)blockIdx.x * kAppendThreads + threadIdx.x;
+  const uint64_t id = (uint64_t)(p.first + blockIdx.x) * kAppendThreads + threadIdx.x;
   const int64_t step = (int64_t)(id / p.units);
   uint32_t piece = (uint32_t)(id % p.units);
   const bool is_v = piece >= p.pieces;
@@ -238,19 +240,25 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(const AppendP
 }
 
 template <bool INT8, bool BF16>
-cwac_status launch_append(const AppendParams &p, hipStream_t st) {
+cwac_status launch_append(AppendParams p, hipStream_t st) {
   // Four tokens to a thread once single ones fill the chip with threads several times.  What those write goes past the caches:
   // 16384 tokens of 8 heads of 128, bf16, 30.4 -> 25.2 us (5.3 TB/s), 4096 tokens (16 MB) 7.5 -> 6.7.  A decoding step's few tokens
   // stay, for the attention behind it.
   const bool many = p.tokens * p.units >= 4 * 262144;
   const int64_t steps = many ? ceil_div(p.tokens, 4) : p.tokens;
   const int64_t blocks = ceil_div(steps * p.units, kAppendThreads);
-  if (blocks > 0x7fffffff) return CWAC_E_SHAPE;
-  if (many)
-    kv_append_kernel<INT8, BF16, 4><<<(unsigned)blocks, kAppendThreads, 0, st>>>(p);
-  else
-    kv_append_kernel<INT8, BF16, 1><<<(unsigned)blocks, kAppendThreads, 0, st>>>(p);
-  return launch_status();
+  static_assert(kAppendThreads == 256, "kAppendBlocksPerLaunch");
+  for (p.first = 0; p.first < blocks; p.first += kAppendBlocksPerLaunch) {
+    const int64_t left = blocks - p.first;
+    const unsigned n = (unsigned)(left < kAppendBlocksPerLaunch ? left : kAppendBlocksPerLaunch);
+    if (many)
+      kv_append_kernel<INT8, BF16, 4><<<n, kAppendThreads, 0, st>>>(p);
+    else
+      kv_append_kernel<INT8, BF16, 1><<<n, kAppendThreads, 0, st>>>(p);
+    const cwac_status s = launch_status();
+    if (s != CWAC_OK) return s;
+  }
+  return CWAC_OK;
 }
 
 bool page_shift(int32_t page, int *shift) {

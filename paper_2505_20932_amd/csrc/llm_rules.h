@@ -1,4 +1,4 @@
-// How the attention over a paged cache is split.  Host arithmetic on sizes only, no HIP: the launcher, the workspace query
+// How the attention over a paged cache is split, and the append's launches.  Host arithmetic on sizes only, no HIP: the launcher, the workspace query
 // and a CPU test share it.
 #pragma once
 
@@ -56,5 +56,8 @@ inline int64_t paged_chunk(int64_t tokens, int splits) {
   const int64_t c = (each + turn - 1) / turn * turn;
   return c < turn ? turn : c;
 }
+
+// Workgroups of one launch of the append (256 threads each; a grid counts fewer than 2^32 threads); more take several.
+constexpr int64_t kAppendBlocksPerLaunch = ((int64_t)1 << 31) / 256;
 
 }  // namespace cwac
