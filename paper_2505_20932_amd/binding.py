@@ -11,6 +11,7 @@ the module cannot be imported."""
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 import warnings
 from typing import Optional
@@ -111,6 +112,17 @@ def _fast_calls():
     return _calls
 
 
+class _int32:
+    """A whole number that has to fit 32 bits (ctypes' own type takes it modulo 2^32)."""
+
+    @staticmethod
+    def from_param(v):
+        v = operator.index(v)
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"{v} is beyond 32 bits")
+        return C.c_int32(v)
+
+
 def lib() -> C.CDLL:
     """Loads the HIP library built in-tree (see build.py); raises if it is absent."""
     global _lib, _calls
@@ -189,6 +201,8 @@ def lib() -> C.CDLL:
             res, args = sig[name]                       # _ex: the same call with a tuning before the stream
             sig[name + "_ex"] = (res, args[:-1] + [tup, vp])
         for name, (res, args) in sig.items():
+            if name.startswith(("llm_", "cwac_mx4_", "qlinear_mx4_")):
+                args = [_int32 if a is i32 else a for a in args]
             fn = getattr(l, name)
             fn.restype, fn.argtypes = res, args
         _lib, _calls = l, _import_fast_calls({name: C.cast(getattr(l, name), vp).value for name in sig})
@@ -568,8 +582,18 @@ def _call(name: str, dev, stream, *args):
     _check(status, name)
 
 
+def _bytes(name: str, *sizes) -> int:
+    """A query's answer; 0, as for all sizes out of range, for those beyond 32 bits."""
+    try:
+        return int(getattr(lib(), name)(*sizes))
+    except C.ArgumentError:
+        if all(isinstance(s, int) for s in sizes):
+            return 0
+        raise
+
+
 def cwac_mx4_scale_bytes(rows: int, k: int) -> int:
-    return int(lib().cwac_mx4_scale_bytes(rows, k))
+    return _bytes("cwac_mx4_scale_bytes", rows, k)
 
 
 def _mx4(codes: torch.Tensor, scales: torch.Tensor, rows: int, k: int):
@@ -682,7 +706,7 @@ def llm_kv_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_cache
 
 
 def llm_paged_attention_workspace(batch: int, q_heads: int, kv_heads: int, head_dim: int, table_cols: int, page: int) -> int:
-    return int(lib().llm_paged_attention_workspace(batch, q_heads, kv_heads, head_dim, table_cols, page))
+    return _bytes("llm_paged_attention_workspace", batch, q_heads, kv_heads, head_dim, table_cols, page)
 
 
 def llm_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scales, v_scales,
