@@ -254,7 +254,8 @@ __global__ __launch_bounds__((64 * PagedCfg<D, I8>::MOST)) void paged_attention_
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           top = fmaxf(top, fmaxf(fabsf(__uint_as_float(fq[s][i] << 16)), fabsf(__uint_as_float(fq[s][i] & 0xffff0000u))));
-      const int e = __builtin_amdgcn_frexp_expf(quad_max(top));
+      // (c < 2^ec stays finite: queries near the largest bfloat16 number are taken relative to less)
+      const int eq = __builtin_amdgcn_frexp_expf(quad_max(top)), ec = __builtin_amdgcn_frexp_expf(c), e = eq < 128 - ec ? eq : 128 - ec;
       c = fmaxf(__builtin_amdgcn_ldexpf(c, e), 0x1p-126f);
 #pragma unroll
       for (int s = 0; s < KS; ++s)

@@ -127,3 +127,31 @@ def test_large_values_lose_their_weight(shape, t, cache, factor):
         special = {i: (3.0 + 0.01 * (i % 7), 2.0 ** factor) for i in low}
         special.update({i: (43.0 + 0.1 * (i % 11), 1.0) for i in high})
         _run(*shape, t, cache, special)
+
+
+@pytest.mark.parametrize("scale", [1.0, -1.0, 8.0, 2.0 ** -3])
+@pytest.mark.parametrize("d,n", [(64, 40), (128, 900), (256, 300)])
+def test_the_largest_bfloat16_queries_over_8_bits(d, n, scale):
+    """Queries of 2^127 over key scales of 2^-125: logits of 64 at most."""
+    g = torch.Generator(device=DEV).manual_seed(n)
+    pages = -(-n // 16)
+    kc = torch.zeros(pages, 1, 16, d, dtype=torch.int8, device=DEV)
+    kc[..., 3] = torch.randint(0, 3, kc.shape[:3], device=DEV, generator=g).to(torch.int8)
+    ks = torch.full(kc.shape[:3], 2.0 ** -125, device=DEV)
+    vc = torch.randint(1, 128, kc.shape, device=DEV, generator=g).to(torch.int8)
+    vs = torch.full(kc.shape[:3], 0.01, device=DEV)
+    q = torch.zeros(1, 2, d, dtype=torch.bfloat16, device=DEV)
+    q[0, 0, 3], q[0, 1, 3] = 2.0 ** 127, -2.0 ** 127
+    q[0, :, 5] = 2.0 ** 120                                            # meets zeros
+    table, lens = torch.arange(pages, dtype=torch.int32, device=DEV)[None].contiguous(), torch.tensor([n], dtype=torch.int32, device=DEV)
+    out = torch.full_like(q, 9.0)
+    ws = torch.empty(max(1, P.llm_paged_attention_workspace(1, 2, 1, d, pages, 16)), dtype=torch.uint8, device=DEV)
+    P.llm_paged_attention(q, kc, vc, ks, vs, table, lens, scale, 0, out, ws)
+    code = kc.transpose(1, 2).reshape(-1, d)[:n, 3].double()
+    v = vc.transpose(1, 2).reshape(-1, d)[:n].double() * vs[0, 0, 0].double()
+    for h, sign in ((0, 1.0), (1, -1.0)):
+        w = torch.softmax(sign * scale * 4.0 * code, dim=0)
+        want = w @ v
+        # the output's rounding; logits of at most 64 in fp32 (two products of 2^-24 each), fp32 sums over n tokens, the two terms of a weight
+        rel = 2.0 ** -8 + 4 * 64 * 2.0 ** -24 + 2.0 ** -23 * (n + 16) + 2.0 ** -20
+        assert ((out[0, h].double() - want).abs() <= want.abs() * rel + n * 2.0 ** -34 * 127 * 0.01).all()
