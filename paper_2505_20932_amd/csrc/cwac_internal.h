@@ -38,9 +38,9 @@ __device__ __forceinline__ float wave_min(float v) {
   return v;
 }
 
-// Between matrix instructions and code that may branch before it reads their results: 16 wait states, as many as a 16 x 16
-// instruction (8 passes) and most of what a 32 x 32 one (16 passes) takes.  The compiler puts the waits in that such a read needs within a
-// block; behind a branch it was seen to leave them out (a result read three instructions after its matrix instruction).
+// Between matrix instructions and code that may branch before it reads their results: 16 wait states, where a 16 x 16 instruction (4
+// passes) takes 8 and a 32 x 32 one (8 passes) 12.  The compiler puts the waits in that such a read needs, but at the target of the first of
+// two branches that end a block it counts the second one as well (a loop's sums, copied where its next turn begins: 7 wait states).
 __device__ __forceinline__ void settle() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_nop 15" ::: "memory");

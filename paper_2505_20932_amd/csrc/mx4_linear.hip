@@ -212,6 +212,7 @@ __global__ __launch_bounds__(64 * W) void mx4_splitk_kernel(const Mx4Params p) {
     wait_lds();  // the unit is in registers, its place is free
     issue(d, first + i + D);
     mma();
+    settle();  // (the next turn may copy the sums)
     d = d + 1 == D ? 0 : d + 1;
   }
   // Memory operations return in order: with r units issued behind a unit, it is complete at r * LPU outstanding.
