@@ -491,7 +491,7 @@ cwac_status cwac_mx4_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t
  *   x_codes, x_scales  [m, k] (activations), w_codes, w_scales [n, k] (weights, nn.Linear layout); ldx, ldw bytes, <= 2^24
  *   m >= 1, n >= 1
  *   mult, fbias        device fp32 [n] or NULL
- *   out                device [m, n], pitch ldo elements; 16-byte aligned rows take whole-line stores, others element-wise ones */
+ *   out                device [m, n], pitch ldo elements; rows may begin at any element */
 cwac_status qlinear_mx4_cwac_forward(const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales, const uint8_t *w_codes,
                                      int64_t ldw, const uint8_t *w_scales, int64_t m, int32_t n, int32_t k,
                                      const float *mult, const float *fbias, int32_t out_kind, void *out, int64_t ldo,
@@ -526,7 +526,8 @@ enum { CWAC_KV_MAX_BATCH = 8192 };
  *   seq_lens     device int32 [batch]: old + new, or old for a request not served
  *   n_left       device int32 [1]: pages left on the stack
  * 1 <= batch <= CWAC_KV_MAX_BATCH; n_free is taken as at most free_capacity.  The call can be repeated on the same
- * inputs; what it writes must not overlap what it reads but for the table (CWAC_E_MODE). */
+ * inputs; what it writes must not overlap what it reads but for the table (CWAC_E_MODE).  Consecutive steps therefore alternate between two pairs of
+ * buffers (one step's seq_lens and n_left are the next one's old_lens and n_free; captured: two graphs in turn), or copy them back. */
 cwac_status llm_kv_assign_pages(const int32_t *old_lens, const int32_t *new_lens, int32_t batch, int32_t page,
                                 const int32_t *free_pages, int32_t free_capacity, const int32_t *n_free, int32_t *table,
                                 int64_t ldt, int32_t table_cols, int64_t *slots, int64_t slot_capacity,
@@ -557,7 +558,10 @@ cwac_status llm_kv_append(const void *k, int64_t ldk, const void *v, int64_t ldv
  *   workspace  device, llm_paged_attention_workspace(...) bytes, 16-byte aligned, for calls in order on one stream: it holds the parts
  *              of split lengths between the call's two launches (calls that may overlap need one each)
  * Logits, maximum, sum and output are accumulated in fp32, a weight meets its value as the sum of two terms: of `type`, over an 8-bit
- * cache of binary16; there bfloat16 queries enter as binary16 numbers relative to a power of two near their head's largest value.
+ * cache of binary16; there bfloat16 queries enter as binary16 numbers relative to a power of two near their head's largest value.  Off by at most
+ *   bfloat16 terms   2^-16 of a weight
+ *   binary16 terms   2^-20 of a weight + 2^-39 of the largest (8 bit: of a weight times its value's scale, 2^-34 of the largest such product)
+ * A logit of minus infinity has weight 0, also where all of them are (zeros); NaN among the visible tokens' numbers comes out as NaN.
  * How a length is split follows from batch, heads, table_cols * page and window alone: a request's result does not depend on the
  * other requests' lengths or contents. */
 size_t llm_paged_attention_workspace(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim,

@@ -2,7 +2,8 @@
 //   o[b, h] = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q[b, h] . k_t - max),  t over the request's visible tokens.
 //
 // Bound: HBM - every visible key and value is read once, 2 to 32 operations per byte (heads that share a key head share
-// the read); 61 requests of up to 8190 tokens, 8 key heads of 128, bf16: 185 us = 5.5 TB/s, int8 with 5 of up to 131072: 165 us, 5.2 TB/s.  So the kernel is a stream:
+// the read); 61 requests of up to 8190 tokens, 8 key heads of 128, bf16: 188 us = 5.4 TB/s, int8 with 5 of up to 131072: 165 us, 5.1 TB/s, the
+// join of the parts another 5 to 6.  So the kernel is a stream:
 //   * a workgroup takes one request, one key head (up to 16 query heads) and a part of the length; its four wavefronts (one,
 //     two or eight where they take a short length whole) take turns over tiles of 32 tokens, each on its own: running maximum, sum and output per
 //     wavefront, joined through LDS at the end and, where the length is split, by a second small kernel through the workspace (fixed
@@ -220,7 +221,7 @@ __global__ __launch_bounds__((64 * PagedCfg<D, I8>::MOST)) void paged_attention_
       for (int i = tid; i < heads * (D / 4); i += 64 * W) reinterpret_cast<u2 *>(out)[i] = u2{0, 0};
     return;
   }
-  // ---- this wavefront's tiles: t0 + wave, + 4, ...
+  // ---- this wavefront's tiles: t0 + wave, + W, ...
   const int t0 = span.first + split * p.split_tiles;
   const int nt = span.tiles - split * p.split_tiles < p.split_tiles ? span.tiles - split * p.split_tiles : p.split_tiles;
   const int mine = (nt - wave + W - 1) >> p.log_waves;  // at least 0

@@ -24,6 +24,9 @@ inline int64_t paged_span(int64_t cap, int window) {
 // splits of 128 tokens or more: 61 requests of 1 to 8190 tokens, 8 key heads, bf16 192 / 189 / 189; 5 of 30011 to 131072, int8
 // 187 / 170 / 164; 256 of 100 to 1900 190 / 190 / 207 (split in two); 8 of 2000, 32 key heads 51 / 52 / 60; 16 of 100 to 8000,
 // heads of 256 101 / 107 / 116; 64 of 100 to 6000, int8 heads of 64 61 / 60 / 53; one of 131072, one key head 17.8 at 128 splits, 19.7 at 256.
+// (The int8 ones take 1 to 3 % more since their weights' unit follows the largest product of weight and scale.)
+// `tokens` is the capacity of a table row, not a request's length: short requests under a wide table get fewer workgroups (61 of up to 8190
+// tokens, 8 key heads: 64 per request under a table of 8192 tokens, 8 under one of 131072).
 inline int paged_splits(int64_t batch, int q_heads, int kv_heads, int64_t tokens) {
   const int group = q_heads / kv_heads, tiles = (group + kPagedHeads - 1) / kPagedHeads;
   const int64_t rows = batch * kv_heads * tiles, turn = kPagedTile * kPagedWaves;

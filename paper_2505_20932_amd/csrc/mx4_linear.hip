@@ -9,8 +9,8 @@
 // panel's eight, one load for all of the panel's steps.
 //
 // K that is no multiple of 256: the last panel's codes beyond K are whatever lies there (the next row, the gap between rows, zeros
-// behind the last row), finite numbers all of them, and their scale bytes are zero on both sides: products of
-// 2^-254 or less, far below half an ulp of any fp32 sum that is not zero and zero when rounded to fp32 by themselves.
+// behind the last row), finite numbers all of them, and their scale bytes are zero on both sides: at most 224 products of
+// 36 * 2^-254, together below 2^-240, far below half an ulp of any fp32 sum that is not zero and zero when rounded to fp32 by themselves.
 #include <type_traits>
 
 #include "mx4.h"
@@ -304,7 +304,7 @@ cwac_status launch_split(Mx4Params p, int out_kind, hipStream_t st) {
 // ------------------------------------------------------------------------------------------
 // Many tiles: BM tokens x BN channels at a time, both panels through a ring of NSTAGE stages in LDS, one stage = one panel of 256
 // values (128 bytes of codes and 8 scale bytes per row).  Bound: the matrix cores, under the device's power limit: 16384 x 4096 x 11008 bf16
-// 333 us = 4.4 PFLOP/s (4.8 over K alone), where the instruction by itself sustains 5.2 on random codes; they are busy for 62 % of
+// 305 to 356 us in the profiler, median 350 = 4.2 PFLOP/s (4.8 over K alone), where the instruction by itself sustains 5.2 on random codes; they are busy for 62 % of
 // the cycles at 1.63 GHz.  128 x 128 tiles read as many LDS cycles as they multiply and take 0.4 us a stage.
 //   * Codes go global -> LDS directly, 8 rows x 128 bytes per load; the 16-byte chunk c of row r lands at position c ^ ((r >> 1) & 7)
 //     (applied on the global side), so operand reads are free of bank conflicts.  Buffer loads whose descriptor moves along K with

@@ -12,7 +12,8 @@ namespace cwac {
 enum { kMx4Split16 = 1, kMx4Split32x16, kMx4Split32, kMx4Split64, kMx4Tile128Deep, kMx4Tile128Pair, kMx4Tile256 };
 
 // Estimated microseconds, fitted to 147 layers of 96 to 8192 tokens (weights cold, P = panels of 256 values of K), the two last to 110
-// layers of 400 to 16384 tokens and any width (off by 9 and 6 % in the mean; the choice costs 1 % over the best).  A round is what the
+// layers of 400 to 16384 tokens and any width (off by 9 and 6 % in the mean, by 17 % at 16384 x 11008 x 4096, 407 for 348, where no
+// other form is near; the choice costs 1 % over the best).  A round is what the
 // chip holds at once: 512 tiles of 32 x 32 (256 of 64 x 64), 256 or 512 of 128 x 128, 256 of 256 x 256.
 //   tokens x channels x K          split 32   split 64   128 deep   128 pair   256      (measured)
 //   128 x 4096 x 4096                 6.1        8.6       11.2       14.5       -
